@@ -37,7 +37,8 @@ typedef enum q8_status {
   Q8_ERR_NONFINITE = 7    /* NaN/Inf where a finite value is required */
 } q8_status;
 
-typedef enum q8_dtype { Q8_U8 = 0, Q8_S8 = 1, Q8_S32 = 2, Q8_F32 = 3 } q8_dtype;
+/* Q8_F16 and Q8_BF16 (IEEE binary16, bfloat16) are types of the token operators only. */
+typedef enum q8_dtype { Q8_U8 = 0, Q8_S8 = 1, Q8_S32 = 2, Q8_F32 = 3, Q8_F16 = 4, Q8_BF16 = 5 } q8_dtype;
 
 /* Which convolution kernel to use. */
 typedef enum q8_conv_algo {
@@ -394,6 +395,93 @@ int q8_detection_output(int n_sources, const float* const* loc, const int* loc_s
                         const float* variances, int N, int classes, int background, float conf_thresh,
                         float nms_thresh, int nms_top_k, int keep_top_k, void* workspace, size_t workspace_bytes,
                         float* d_out, int* d_counts, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Token operators (the paper has no counterpart): the 8-bit products of language models, whose activations have no
+ * calibrated factor.  A tensor of activations is a matrix of tokens (rows) by channels with a row pitch in elements
+ * (ldx >= C: a slice of a wider tensor will do); each token carries a factor of its own, found from its values when
+ * it is quantized, and each output channel of a weight matrix [K][C] its own, max|w[k]| / 127 (q8_calibrate_maxabs_rows,
+ * q8_factor, q8_quantize_rows).
+ * ---------------------------------------------------------------------- */
+
+/* Codes and factors of `tokens` rows of C values of x_type (Q8_F32, Q8_F16 or Q8_BF16, converted to fp32 exactly):
+ *   m = max_c |x[t][c]|,  s[t] = 1 if m == 0, else max(m / 127, 2^-126)   (one fp32 division)
+ *   z[t][c] = clamp(Round(x[t][c] / s[t]), -128, 127)                      (fp32 IEEE division, half to even)
+ * A token with a NaN or an infinity has factor NaN and codes 0, so that what is computed from it is NaN and other tokens
+ * are untouched.  x: device [tokens][ldx].  z: device s8 [tokens][ldz]; only the C codes of a row are written.  d_scale:
+ * device fp32 [tokens].  Any alignment (x to its element); rows on the 16-byte grid are faster.  x and z may not overlap.
+ * tokens == 0 is allowed.  Errors: Q8_ERR_INVALID_ARG (null pointer, C == 0, ldx or ldz < C, bad type), Q8_ERR_ALIGNMENT
+ * (x not aligned to its element, d_scale to 4 bytes), Q8_ERR_CUDA. */
+int q8_quantize_tokens(const void* x, int x_type, size_t tokens, size_t C, size_t ldx, int8_t* z, size_t ldz,
+                       float* d_scale, void* stream);
+
+/* r[t][c] = s[t] * float(z[t][c]): one fp32 product, rounded once to r_type (Q8_F32, Q8_F16 or Q8_BF16).  Arguments as
+ * above. */
+int q8_dequantize_tokens(const int8_t* z, size_t tokens, size_t C, size_t ldz, const float* d_scale, void* r, int r_type,
+                         size_t ldr, void* stream);
+
+/* Product of a token matrix with a weight matrix in 8-bit integers, a factor per token and per output channel:
+ *   acc = sum_c z[t][c] * w[k][c]                                  (int32, exact: C <= 131071)
+ *   y[t][k] = (float(acc) * x_scale[t]) * w_scale[k] (+ bias[k])   (fp32, each step rounded once; then rounded to y_type)
+ * x_type Q8_S8: x holds codes and x_scale their factors.  x_type Q8_F32, Q8_F16 or Q8_BF16: x holds activations, which the
+ * call turns into codes and factors as q8_quantize_tokens does (x_scale NULL). */
+typedef struct q8_linear_desc {
+  int64_t ldx, ldw, ldy;    /* elements from one row to the next; 0: C, C, K */
+  int32_t M, C, K;          /* tokens, input channels, output channels */
+  int32_t x_type;           /* Q8_S8, Q8_F32, Q8_F16 or Q8_BF16 */
+  int32_t y_type;           /* Q8_F32, Q8_F16 or Q8_BF16 */
+  int32_t reserved;         /* 0 */
+} q8_linear_desc;
+
+/* Bytes of device scratch with which q8_linear runs `d` fastest, given 16-byte aligned pointers (0 for many): the codes
+ * and factors of floating-point activations, and copies on the 16-byte grid of codes and weights off it.  Host only. */
+int q8_linear_workspace_bytes(const q8_linear_desc* d, size_t* bytes);
+
+/* x: device [M][ldx] (x_type).  x_scale: device fp32 [M] or NULL (see above).  w: device s8 [K][ldw].  w_scale: device fp32
+ * [K].  bias: device fp32 [K] or NULL.  y: device [M][ldy] (y_type); only the K values of a row are written; may not overlap
+ * an input.  workspace: device, 16-byte aligned, workspace_bytes long, or NULL: with less than q8_linear_workspace_bytes()
+ * the result is the same, slower.  Its contents are undefined afterwards; calls that may overlap on the GPU need one
+ * each.  M == 0 is allowed.  Alignment: elements, and 16 bytes (pointers and pitches) for the fast paths.
+ * Errors: Q8_ERR_INVALID_ARG (null pointer, extents, pitches, types, C > 131071), Q8_ERR_ALIGNMENT (a pointer not aligned to
+ * its element, a workspace off 16 bytes), Q8_ERR_CUDA.  Nothing is launched on an argument error. */
+int q8_linear(const q8_linear_desc* d, const void* x, const float* x_scale, const int8_t* w, const float* w_scale,
+              const float* bias, void* y, void* workspace, size_t workspace_bytes, void* stream);
+
+/* A mixture-of-experts layer for a few tokens: router, choice of the experts, their gated layers with 8-bit weights, sum.
+ *   l[t][e] = sum_c x[t][c] * router[e][c]                               (formed in 64 bits)
+ *   the top_k experts of largest l, best first; ties to the lower index; a NaN ranks below everything
+ *   p = softmax of the token's l, over the chosen experts (renormalize 1) or over all of them (0)
+ *   g = (x . w_gate_up[e][i]) * s_gate_up[e][i],  u = (x . w_gate_up[e][I + i]) * s_gate_up[e][I + i],  i < I
+ *   h[i] = g / (1 + exp(-g)) * u
+ *   y[t][c] = sum over the chosen e of p * ((h . w_down[e][c]) * s_down[e][c])
+ * Activations and h are not rounded to 8 bits: they keep at least 22 bits below the largest of their row, and results are
+ * those of 32-bit arithmetic.  The same inputs give the same bits whatever the other tokens of the call are. */
+typedef struct q8_moe_desc {
+  int64_t ldx, ldy;         /* elements from one token to the next; 0: C */
+  int32_t T, C, I, E;       /* tokens, width, inner width of an expert, experts */
+  int32_t top_k;            /* experts of a token */
+  int32_t x_type;           /* of x and y: Q8_F32, Q8_F16 or Q8_BF16 */
+  int32_t renormalize;      /* 0/1 */
+  int32_t reserved;         /* 0 */
+} q8_moe_desc;
+
+/* Device scratch q8_moe needs for `d` (a multiple of 256 bytes).  Host only. */
+int q8_moe_workspace_bytes(const q8_moe_desc* d, size_t* bytes);
+
+/* x: device [T][ldx].  router: device fp32 [E][C].  w_gate_up: device s8 [E][2 I][C], an expert's gate rows before its up
+ * rows; s_gate_up: device fp32 [E][2 I].  w_down: device s8 [E][C][I]; s_down: device fp32 [E][C].  y: device [T][ldy], of
+ * which the C values of a row are written; may not overlap an input.  ids: device s32 [T][top_k] or NULL, the chosen experts;
+ * probs: device fp32 [T][top_k] or NULL, their p.  workspace: device, 256-byte aligned; contents undefined before and after;
+ * calls that may overlap on the GPU need one each.  T == 0 is allowed.  Any T runs, tokens in groups of 16, each of which
+ * reads the weights of its experts: meant for few tokens.  Weights whose rows lie on the 16-byte grid (C and I multiples
+ * of 16, pointers aligned) are faster.
+ * Limits: C, I <= 131071, E <= 1024, top_k <= min(E, 32).
+ * Errors: Q8_ERR_INVALID_ARG (null pointer, extents, pitches, types), Q8_ERR_UNSUPPORTED (a limit), Q8_ERR_ALIGNMENT (a
+ * pointer not aligned to its element, the workspace off 256 bytes), Q8_ERR_WORKSPACE, Q8_ERR_CUDA.  Nothing is launched on
+ * an argument error. */
+int q8_moe(const q8_moe_desc* d, const void* x, const float* router, const int8_t* w_gate_up, const float* s_gate_up,
+           const int8_t* w_down, const float* s_down, void* y, int32_t* ids, float* probs, void* workspace,
+           size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

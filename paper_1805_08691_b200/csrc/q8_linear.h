@@ -1,0 +1,24 @@
+// Declarations shared by the translation units of q8_linear (host side).
+#pragma once
+#include "q8_internal.h"
+
+namespace q8 {
+
+struct LinearArgs {
+  int M, C, K;
+  long long ldx, ldw, ldy;
+  int x_type, y_type;
+  const void* x;
+  const float* x_scale;
+  const int8_t* w;
+  const float* w_scale;
+  const float* bias;
+  void* y;
+  cudaStream_t stream;
+};
+
+// Few tokens, or operands off the 16-byte grid: weights streamed row by row (q8_linear_rows.cu).
+int launch_linear_rows(const LinearArgs& a);
+int launch_quantize_tokens(const void* x, int x_type, size_t tokens, size_t C, size_t ldx, int8_t* z, size_t ldz, float* scale, cudaStream_t s);
+
+}  // namespace q8
