@@ -17,6 +17,8 @@ struct LinearArgs {
   cudaStream_t stream;
 };
 
+// Many tokens, codes on the 16-byte grid: tensor cores fed by TMA (q8_linear_umma.cu).
+int launch_linear_umma(const LinearArgs& a);
 // Few tokens, or operands off the 16-byte grid: weights streamed row by row (q8_linear_rows.cu).
 int launch_linear_rows(const LinearArgs& a);
 int launch_quantize_tokens(const void* x, int x_type, size_t tokens, size_t C, size_t ldx, int8_t* z, size_t ldz, float* scale, cudaStream_t s);

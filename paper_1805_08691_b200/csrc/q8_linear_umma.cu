@@ -1,0 +1,311 @@
+// The product with a factor per token on the tensor cores, for many tokens.
+//
+//   D[256 tokens, BN output channels] (int32, TMEM) = Z[256, C] (s8, TMA) x W[BN, C]^T (s8, TMA)
+//
+// Persistent pairs of CTAs (clusters of two), tcgen05.mma.cta_group::2.kind::i8, 256 x BN x 32 an instruction: each CTA
+// loads its 128 rows of codes and half of the weight rows, 128 bytes of the reduction a stage, and holds 128 rows of the
+// accumulator; the leader issues.  Two accumulators alternate, so that one tile's results are scaled and stored while the
+// next tile is multiplied.
+//
+// Roles of a CTA: warp 0 loads, warp 1 issues (leader) and owns the TMEM, warps 2 to 9 scale and store: thread = accumulator
+// row (token), the two groups of four warps take half of the columns each.  All waits are bounded.
+#include <type_traits>
+
+#include "q8_linear.h"
+#include "q8_token_common.cuh"
+#include "q8_umma_common.cuh"
+
+namespace q8 {
+namespace {
+
+constexpr int kLBK = 128;                      // bytes of the reduction per stage
+constexpr int kLEpiWarps = 8, kLThreads = 64 + 32 * kLEpiWarps;
+constexpr int kLMaxStages = 8;
+constexpr unsigned kLABytes = 128 * kLBK;
+
+struct LinearParams {
+  int M, K;
+  int bn, kblocks, stages, m_tiles, n_tiles;
+  FastDiv fd_group, fd_rows;  // see tile_of
+  int group;
+  unsigned stage_bytes, idesc, desc_hi;
+  const float* x_scale;
+  const float* w_scale;
+  const float* bias;
+  void* y;
+  long long ldy;
+  int y_vec;                  // rows of y on the 16-byte grid
+  unsigned* status;
+};
+
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t leader_bar, int c0, int c1) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(dst), "l"(map), "r"(leader_bar), "r"(c0), "r"(c1)
+      : "memory");
+}
+
+// Tiles in bands of `group` token tiles, all output channels of a band before the next: what runs at a time then covers a
+// near-square part of the result, whose operands the L2 holds.
+__device__ __forceinline__ void tile_of(const LinearParams& p, int tile, int* mt, int* nt) {
+  const int band = p.fd_group.div(tile), first = band * p.group, in = tile - band * p.fd_group.d;
+  const int rows = min(p.group, p.m_tiles - first);
+  const int n = rows == p.group ? p.fd_rows.div(in) : in / rows;
+  *nt = n;
+  *mt = first + in - n * rows;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_16(T* y, const float (&v)[16], int valid, bool vec) {
+  if (vec && valid >= 16) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) reinterpret_cast<float4*>(y)[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    } else {
+      unsigned w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (std::is_same<T, __half>::value) {
+          const __half2 h = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+          w[j] = *reinterpret_cast<const unsigned*>(&h);
+        } else {
+          const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+          w[j] = *reinterpret_cast<const unsigned*>(&h);
+        }
+      }
+      reinterpret_cast<uint4*>(y)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      reinterpret_cast<uint4*>(y)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (j < valid) y[j] = from_f32<T>(v[j]);
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kLThreads, 1) __cluster_dims__(2, 1, 1)
+    linear_umma_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ LinearParams p) {
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) unsigned long long full[kLMaxStages], empty[kLMaxStages], acc_full[2], acc_empty[2];
+  __shared__ __align__(16) float s_scale[2][256], s_bias[2][256];
+  __shared__ uint32_t tmem_holder;
+  __shared__ int abort_flag;
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  const int rank = __shfl_sync(0xffffffffu, (int)cluster_ctarank(), 0);
+  const int first = (int)(blockIdx.x >> 1), step = (int)(gridDim.x >> 1), tiles = p.m_tiles * p.n_tiles;
+  const int half = p.bn >> 1;  // weight rows of a CTA
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (warp == 0) {
+    if (lane < p.stages) { mbar_init(smem_u32(&full[lane]), 1); mbar_init(smem_u32(&empty[lane]), 1); }
+    else if (lane >= 16 && lane < 18) { mbar_init(smem_u32(&acc_full[lane - 16]), 1); mbar_init(smem_u32(&acc_empty[lane - 16]), 2 * kLEpiWarps); }
+    else if (lane == 18) abort_flag = 0;
+    else if (lane == 19) prefetch_tensormap(&tmX);
+    else if (lane == 20) prefetch_tensormap(&tmW);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  } else if (warp == 1) {
+    tmem_alloc_pair(smem_u32(&tmem_holder), 512);
+    tmem_relinquish_pair();
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tcgen05_fence_after();
+  const uint32_t tmem = tmem_holder;
+  volatile int* abortp = &abort_flag;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  int issued = 0;  // stages loaded (warp 0)
+  if (warp == 0) {
+    uint32_t stage = 0, phase = 1;
+    bool ok = true;
+    for (int tile = first; tile < tiles && ok; tile += step) {
+      int mt, nt;
+      tile_of(p, tile, &mt, &nt);
+      const int m0 = mt * 256 + rank * 128, n0 = nt * p.bn + rank * half;
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        if (!mbar_wait(smem_u32(&empty[stage]), phase, abortp)) { ok = false; break; }
+        if (elect_one()) {
+          const uint32_t bar = smem_u32(&full[stage]), lbar = map_to_cta(bar, 0), dst = base + stage * p.stage_bytes;
+          if (rank == 0) mbar_arrive_expect_tx(bar, 2u * p.stage_bytes);
+          tma_load_2d_pair(dst, &tmX, lbar, kb * kLBK, m0);
+          tma_load_2d_pair(dst + kLABytes, &tmW, lbar, kb * kLBK, n0);
+        }
+        ++issued;
+        if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+      }
+    }
+    if (!ok && lane == 0) { abort_flag = 1; atomicOr(p.status, kTimeoutProducer); }
+  } else if (warp == 1) {
+    if (rank == 0) {
+      uint32_t stage = 0, phase = 0, ab = 0, apar = 1;
+      bool ok = true;
+      for (int tile = first; tile < tiles && ok; tile += step) {
+        if (!mbar_wait(smem_u32(&acc_empty[ab]), apar, abortp)) { ok = false; break; }
+        tcgen05_fence_after();
+        const uint32_t d = tmem + ab * 256u;
+        for (int kb = 0; kb < p.kblocks; ++kb) {
+          if (!mbar_wait(smem_u32(&full[stage]), phase, abortp)) { ok = false; break; }
+          tcgen05_fence_after();
+          if (elect_one()) {
+            const uint32_t at = base + stage * p.stage_bytes;
+            const uint32_t a = kDescLbo | ((at >> 4) & 0x3fffu), b = kDescLbo | (((at + kLABytes) >> 4) & 0x3fffu);
+            umma_i8_pair(d, a, b, p.desc_hi, p.idesc, kb ? 1u : 0u);
+            umma_i8_pair(d, a + 2, b + 2, p.desc_hi, p.idesc, 1u);
+            umma_i8_pair(d, a + 4, b + 4, p.desc_hi, p.idesc, 1u);
+            umma_i8_pair(d, a + 6, b + 6, p.desc_hi, p.idesc, 1u);
+            umma_commit_pair(smem_u32(&empty[stage]));
+          }
+          if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+        }
+        if (ok && elect_one()) umma_commit_pair(smem_u32(&acc_full[ab]));
+        ab ^= 1u;
+        if (ab == 0) apar ^= 1u;
+      }
+      if (!ok && lane == 0) { abort_flag = 1; atomicOr(p.status, kTimeoutMma); }
+    }
+  } else {
+    const int e = warp - 2, quad = warp & 3, group = e >> 2, tid = (int)threadIdx.x - 64;
+    const int chunks = p.bn >> 4, per = (chunks + 1) >> 1, c0 = group * per, c1 = min(chunks, c0 + per);
+    uint32_t ab = 0, par = 0;
+    bool ok = true;
+    for (int tile = first; tile < tiles; tile += step) {
+      int mt, nt;
+      tile_of(p, tile, &mt, &nt);
+      const int n0 = nt * p.bn;
+      const long long m = (long long)mt * 256 + rank * 128 + quad * 32 + lane;
+      const bool live = m < p.M;
+      const float sx = live ? p.x_scale[m] : 0.0f;
+      if (tid < p.bn) {
+        const int n = n0 + tid;
+        s_scale[ab][tid] = n < p.K ? p.w_scale[n] : 0.0f;
+        s_bias[ab][tid] = p.bias && n < p.K ? p.bias[n] : 0.0f;
+      }
+      asm volatile("bar.sync 2, %0;" ::"n"(32 * kLEpiWarps) : "memory");
+      if (ok && !mbar_wait(smem_u32(&acc_full[ab]), par, abortp)) {
+        ok = false;
+        if (lane == 0) { abort_flag = 1; atomicOr(p.status, kTimeoutEpilogue); }
+      }
+      if (!ok) continue;  // the other warps may still meet this one at the barrier above
+      tcgen05_fence_after();
+      const uint32_t t = tmem + ab * 256u + ((uint32_t)quad << 21);
+      T* row = static_cast<T*>(p.y) + m * p.ldy + n0;
+      auto chunk = [&](const int (&acc)[16], int c) {
+        float f[16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float4 s = *reinterpret_cast<const float4*>(&s_scale[ab][c * 16 + 4 * j]);
+          f[4 * j] = __fmul_rn(__fmul_rn(__int2float_rn(acc[4 * j]), sx), s.x);
+          f[4 * j + 1] = __fmul_rn(__fmul_rn(__int2float_rn(acc[4 * j + 1]), sx), s.y);
+          f[4 * j + 2] = __fmul_rn(__fmul_rn(__int2float_rn(acc[4 * j + 2]), sx), s.z);
+          f[4 * j + 3] = __fmul_rn(__fmul_rn(__int2float_rn(acc[4 * j + 3]), sx), s.w);
+        }
+        if (p.bias) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) f[j] = __fadd_rn(f[j], s_bias[ab][c * 16 + j]);
+        }
+        if (live) store_16(row + c * 16, f, p.K - n0 - c * 16, p.y_vec);
+      };
+      int va[16], vb[16];
+      if (c0 < c1) tmem_ld_16(t + c0 * 16, va);
+#pragma unroll 1
+      for (int c = c0; c < c1; c += 2) {
+        tmem_ld_wait(va);
+        if (c + 1 < c1) tmem_ld_16(t + (c + 1) * 16, vb);
+        chunk(va, c);
+        if (c + 1 < c1) {
+          tmem_ld_wait(vb);
+          if (c + 2 < c1) tmem_ld_16(t + (c + 2) * 16, va);
+          chunk(vb, c + 1);
+        }
+      }
+      tcgen05_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&acc_empty[ab]), 0));
+      ab ^= 1u;
+      if (ab == 0) par ^= 1u;
+    }
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  // After a wait that gave up, loads may still be on their way into this CTA's or its peer's shared memory.
+  if (warp == 0 && rank == 0 && *abortp) {
+    int never = 0;
+    for (int i = max(0, issued - p.stages); i < issued; ++i)
+      mbar_wait_slow(smem_u32(&full[i % p.stages]), (uint32_t)(i / p.stages) & 1u, &never, 100000000ull);
+  }
+  cluster_sync_all();
+  if (warp == 1) {
+    tcgen05_fence_after();
+    tmem_dealloc_pair(tmem, 512);
+  }
+}
+
+int encode_rows_map(CUtensorMap* map, const void* base, long long ld, int C, long long rows, int box_rows) {
+  const DriverFns& fn = driver_fns();
+  if (!fn.tiled) return fail(Q8_ERR_CUDA, "linear_umma: cuTensorMapEncodeTiled entry point not available");
+  cuuint64_t dims[2] = {(cuuint64_t)C, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+  cuuint32_t box[2] = {(cuuint32_t)kLBK, (cuuint32_t)box_rows}, ones[2] = {1, 1};
+  const CUresult r = fn.tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(Q8_ERR_CUDA, "linear_umma: tensor map rejected (CUresult %d)", (int)r);
+  return Q8_OK;
+}
+
+template <typename T>
+int launch_pairs(const CUtensorMap& tmX, const CUtensorMap& tmW, const LinearParams& p, int grid, size_t dyn, cudaStream_t s) {
+  static std::atomic<bool> set[kMaxDevices];
+  const int dev = current_device();
+  if (dev < 0 || !set[dev].load(std::memory_order_relaxed)) {
+    const int rc = check_cuda(cudaFuncSetAttribute(linear_umma_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit - 8192), "linear_umma_kernel");
+    if (rc != Q8_OK) return rc;
+    if (dev >= 0) set[dev].store(true, std::memory_order_relaxed);
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(kLThreads);
+  cfg.dynamicSmemBytes = dyn;
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return check_cuda(cudaLaunchKernelEx(&cfg, linear_umma_kernel<T>, tmX, tmW, p), "linear_umma_kernel");
+}
+
+}  // namespace
+
+int launch_linear_umma(const LinearArgs& a) {
+  LinearParams p{};
+  p.M = a.M; p.K = a.K;
+  p.kblocks = (a.C + kLBK - 1) / kLBK;
+  p.m_tiles = (int)(((long long)a.M + 255) / 256);
+  p.bn = 256;
+  p.n_tiles = (a.K + p.bn - 1) / p.bn;
+  p.group = p.m_tiles < 8 ? p.m_tiles : 8;
+  p.fd_group = make_fastdiv(p.group * p.n_tiles);
+  p.fd_rows = make_fastdiv(p.group);
+  p.stage_bytes = kLABytes + (unsigned)(p.bn / 2) * kLBK;
+  p.stages = 6;
+  p.idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((unsigned)(p.bn >> 3) << 17) | ((256u >> 4) << 24);
+  p.desc_hi = (unsigned)((8 * kLBK) >> 4) | (1u << 14) | (2u << 29);
+  p.x_scale = a.x_scale; p.w_scale = a.w_scale; p.bias = a.bias;
+  p.y = a.y; p.ldy = a.ldy;
+  p.y_vec = aligned16(a.y) && a.ldy * (long long)type_bytes(a.y_type) % 16 == 0;
+  p.status = status_word_device_ptr();
+  if (!p.status) return fail(Q8_ERR_CUDA, "linear_umma: status word not available");
+  CUtensorMap tmX, tmW;
+  int rc = encode_rows_map(&tmX, a.x, a.ldx, a.C, a.M, 128);
+  if (rc == Q8_OK) rc = encode_rows_map(&tmW, a.w, a.ldw, a.C, a.K, p.bn / 2);
+  if (rc != Q8_OK) return rc;
+  const long long tiles = (long long)p.m_tiles * p.n_tiles, pairs = sm_count() / 2;
+  const int grid = 2 * (int)(tiles < pairs ? tiles : pairs);
+  const size_t dyn = 1024 + (size_t)p.stages * p.stage_bytes;
+  if (a.y_type == Q8_F32) return launch_pairs<float>(tmX, tmW, p, grid, dyn, a.stream);
+  if (a.y_type == Q8_F16) return launch_pairs<__half>(tmX, tmW, p, grid, dyn, a.stream);
+  return launch_pairs<__nv_bfloat16>(tmX, tmW, p, grid, dyn, a.stream);
+}
+
+}  // namespace q8
