@@ -18,6 +18,7 @@
 // Blocks that wait hold a ticket of phase two, so that all items of phase one are in the hands of running blocks: progress
 // needs no co-residency.  Waits are bounded all the same.
 #include <atomic>
+#include <cmath>
 #include <type_traits>
 
 #include "q8_token_common.cuh"
@@ -26,6 +27,7 @@ namespace q8 {
 namespace {
 
 constexpr int kMoeGroup = 16;    // tokens of a pass
+constexpr int kMoeRows = 256;    // ... times top_k, at most
 constexpr int kMoeWarps = 16, kMoeThreads = 32 * kMoeWarps;
 constexpr int kMaxTopK = 32;      // a lane each
 constexpr int kMaxExperts = 1024; // a bit of a lane's word each
@@ -33,6 +35,12 @@ constexpr int kAccPitch = 20;    // ints between two columns of accumulators: la
 constexpr float kDigitMax = 8355711.0f;  // 127 (256^2 + 256 + 1)
 constexpr unsigned kTimeoutMoe = 32u;
 constexpr unsigned long long kMoeWaitNs = 2000000000ull;
+
+// Division of 0 <= x < 2^31 by a number known to the host (Granlund and Montgomery, PLDI 1994).
+struct Divide {
+  unsigned m, l;
+  __device__ __forceinline__ int operator()(int x) const { return (int)((__umulhi((unsigned)x, m) + (unsigned)x) >> l); }
+};
 
 struct MoeParams {
   int T, C, I, E, k, renormalize, x_type;
@@ -50,12 +58,15 @@ struct MoeParams {
   double* logits;        // [T][E]
   float* x_factor;       // [T]
   float* h_factor;       // [T k]
-  unsigned* sync;        // two tickets, then per chosen expert the finished items and the flag
+  unsigned* sync;        // two tickets; per chosen expert the finished items, then the flags; finished items per tile
+  float* part;           // weighted results of the experts [T k][C]
   signed char* xd;       // digits of the tokens [T][3][x_pitch]
   signed char* hd;       // digits of the inner activations [T k][3][h_pitch]
-  float* h;              // inner activations [T k][I]
+  float* h;              // inner activations [T k][h_pitch]
   int x_pitch, h_pitch;  // multiples of 128
-  int unit_blocks, tiles;
+  int unit_blocks, tiles, steps;  // items of an expert in phase one; items of phase two; steps of an item of phase one
+  int ks[2];                      // warps that share the reduction of an item, by phase
+  Divide by_unit_blocks, by_tiles;
   int x_vec, r_vec;
   unsigned* status;
 };
@@ -124,7 +135,7 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if ((int)blockIdx.x < p.T) {  // digits of a token
     const int t = blockIdx.x;
-    if (t == 0) for (int i = threadIdx.x; i < 2 + 2 * min(p.E, p.T * p.k); i += 256) p.sync[i] = 0u;
+    if (t == 0) for (int i = threadIdx.x; i < 2 + 2 * min(p.E, p.T * p.k) + p.tiles; i += 256) p.sync[i] = 0u;
     __shared__ unsigned part[8];
     unsigned m = 0;
     if (p.x_vec) {
@@ -161,27 +172,50 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
     }
     return;
   }
-  const int pair = ((int)blockIdx.x - p.T) * 8 + warp;
-  if (pair >= p.T * p.E) return;
-  const int e = pair / p.T, t = pair - e * p.T;
+  // all tokens' logits of an expert; a thread's share of the channels does not depend on their number
+  __shared__ double part_sum[8][kMoeGroup];
+  const int e = (int)blockIdx.x - p.T;
   const float* r = p.router + (size_t)e * p.C;
-  double s0 = 0.0, s1 = 0.0;
+  double s[kMoeGroup];
+#pragma unroll
+  for (int t = 0; t < kMoeGroup; ++t) s[t] = 0.0;
   if (p.x_vec && p.r_vec) {
-#pragma unroll 4
-    for (int c = 4 * lane; c < p.C; c += 128) {
-      const float4 v = load_x4(p, t, c), w = __ldg(reinterpret_cast<const float4*>(r + c));
-      s0 = __fma_rn((double)v.x, (double)w.x, s0);
-      s1 = __fma_rn((double)v.y, (double)w.y, s1);
-      s0 = __fma_rn((double)v.z, (double)w.z, s0);
-      s1 = __fma_rn((double)v.w, (double)w.w, s1);
+    for (int c = 4 * threadIdx.x; c < p.C; c += 1024) {
+      const float4 w = __ldg(reinterpret_cast<const float4*>(r + c));
+#pragma unroll
+      for (int t = 0; t < kMoeGroup; ++t) {
+        if (t >= p.T) break;
+        const float4 v = load_x4(p, t, c);
+        s[t] = __fma_rn((double)v.x, (double)w.x, s[t]);
+        s[t] = __fma_rn((double)v.y, (double)w.y, s[t]);
+        s[t] = __fma_rn((double)v.z, (double)w.z, s[t]);
+        s[t] = __fma_rn((double)v.w, (double)w.w, s[t]);
+      }
     }
   } else {
-    for (int c = lane; c < p.C; c += 32) s0 = __fma_rn((double)load_x(p, t, c), (double)r[c], s0);
-  }
-  s0 += s1;
+    for (int c = threadIdx.x; c < p.C; c += 256) {
+      const double w = (double)r[c];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s0 += __shfl_xor_sync(0xffffffffu, s0, o);
-  if (lane == 0) p.logits[(size_t)t * p.E + e] = s0;
+      for (int t = 0; t < kMoeGroup; ++t) {
+        if (t >= p.T) break;
+        s[t] = __fma_rn((double)load_x(p, t, c), w, s[t]);
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < kMoeGroup; ++t) {
+    if (t >= p.T) break;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s[t] += __shfl_xor_sync(0xffffffffu, s[t], o);
+    if (lane == 0) part_sum[warp][t] = s[t];
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < p.T) {
+    double l = part_sum[0][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) l += part_sum[w][threadIdx.x];
+    p.logits[(size_t)threadIdx.x * p.E + e] = l;
+  }
 }
 
 // ------------------------------------------------------------------------------------------ experts
@@ -191,7 +225,10 @@ __device__ __forceinline__ unsigned long long order_key(double v) {
   const long long b = __double_as_longlong(v == 0.0 ? 0.0 : v);
   return b < 0 ? ~(unsigned long long)b : (unsigned long long)b | 0x8000000000000000ull;
 }
-
+__device__ __forceinline__ double key_value(unsigned long long k) {
+  if (k == 0ull) return __longlong_as_double(0x7ff8000000000000ll);
+  return __longlong_as_double((long long)(k >> 63 ? k & 0x7fffffffffffffffull : ~k));
+}
 // What a block knows of the choice of experts; rows: (token, chosen expert) pairs by expert, then token.
 struct MoeChoice {
   int* expert;          // [rows] experts some token has chosen, ascending
@@ -200,6 +237,7 @@ struct MoeChoice {
   float* prob;          // [rows] by row
   int* row_of;          // [T][k] rows of a token, ascending
   int* row_expert;      // [rows]
+  int* row_token;       // [rows]
 };
 
 __device__ __forceinline__ int load_acquire(const unsigned* p) {
@@ -230,182 +268,385 @@ __device__ __noinline__ bool wait_raised(const unsigned* flag, volatile int* gav
   }
 }
 
-// Sixteen bytes pos .. of a weight row, for the row's alignment kGrid (16, 8 or 1 bytes), zero from `len` on.  Rows off the
-// grid are read in aligned words, each of which holds a byte of the row.
+// Sixteen bytes of a weight row as they are loaded, zero from the row's end on.  kGrid: 16 or 8, the alignment of every row,
+// or 1: rows anywhere, read as aligned words each of which holds a byte of the row.  `left`: bytes of the row from `at` on.
 template <int kGrid>
-__device__ __forceinline__ uint4 load_weights(const signed char* row, int pos, int len) {
-  uint4 v = make_uint4(0u, 0u, 0u, 0u);
-  if (kGrid == 16) {
-    if (pos < len)
-      asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + pos));
-  } else if (kGrid == 8) {
-    if (pos < len) { const uint2 a = __ldg(reinterpret_cast<const uint2*>(row + pos)); v.x = a.x; v.y = a.y; }
-    if (pos + 8 < len) { const uint2 a = __ldg(reinterpret_cast<const uint2*>(row + pos + 8)); v.z = a.x; v.w = a.y; }
+struct Bytes16 {
+  unsigned w[kGrid == 1 ? 5 : 4];
+};
+template <int kGrid>
+__device__ __forceinline__ void load_bytes(Bytes16<kGrid>& v, const signed char* at, int left) {
+#pragma unroll
+  for (int k = 0; k < (kGrid == 1 ? 5 : 4); ++k) v.w[k] = 0u;
+  if constexpr (kGrid == 16) {
+    if (left > 0) asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "l"(at));
+  } else if constexpr (kGrid == 8) {
+    if (left > 0) asm volatile("ld.global.nc.v2.u32 {%0, %1}, [%2];" : "=r"(v.w[0]), "=r"(v.w[1]) : "l"(at));
+    if (left > 8) asm volatile("ld.global.nc.v2.u32 {%0, %1}, [%2];" : "=r"(v.w[2]), "=r"(v.w[3]) : "l"(at + 8));
   } else {
-    const unsigned long long at = (unsigned long long)(row + pos);
-    const unsigned* w = reinterpret_cast<const unsigned*>(at & ~3ull);
-    const int m = (int)(at & 3ull);
-    unsigned u[5];
+    const unsigned* w = reinterpret_cast<const unsigned*>((unsigned long long)at & ~3ull);
+    const int m = (int)((unsigned long long)at & 3ull);
 #pragma unroll
-    for (int k = 0; k < 5; ++k) u[k] = pos + 4 * k - m < len && (k < 4 || m > 0) ? __ldg(w + k) : 0u;
-    v.x = __funnelshift_r(u[0], u[1], 8 * m);
-    v.y = __funnelshift_r(u[1], u[2], 8 * m);
-    v.z = __funnelshift_r(u[2], u[3], 8 * m);
-    v.w = __funnelshift_r(u[3], u[4], 8 * m);
-  }
-  return v;
-}
-
-// Columns of the digits of an expert's tokens for this lane: byte offsets of the rows it reads.
-template <int NT>
-__device__ __forceinline__ void column_offsets(unsigned tokens, int count, int first_row, int pitch, bool by_row, int lane, unsigned (&off)[NT]) {
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int col = 8 * t + (lane >> 2), r = min(col / 3, count - 1), d = col - col / 3 * 3;
-    const int row = by_row ? first_row + r : (int)__fns(tokens, 0, r + 1);
-    off[t] = (unsigned)(row * 3 + d) * (unsigned)pitch + 16u * (lane & 3);
+    for (int k = 0; k < 5; ++k)
+      if (4 * k - m < left && (k < 4 || m > 0)) asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v.w[k]) : "l"(w + k));
   }
 }
+template <int kGrid>
+__device__ __forceinline__ uint4 whole_bytes(const Bytes16<kGrid>& v, int shift) {
+  if constexpr (kGrid != 1) return make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+  else return make_uint4(__funnelshift_r(v.w[0], v.w[1], shift), __funnelshift_r(v.w[1], v.w[2], shift), __funnelshift_r(v.w[2], v.w[3], shift),
+                         __funnelshift_r(v.w[3], v.w[4], shift));
+}
 
-// Partial products of 16 weight rows (this lane's are wa and wb) with 8 NT columns over the steps [s0, s1) of 64 bytes,
-// added to acc[column][16] in shared memory.  `wait`: called once, with the first weights on their way.
-template <int NT, int kGrid, typename Wait>
-__device__ __forceinline__ void stream_rows(const signed char* wa, const signed char* wb, int len, const signed char* cols, const unsigned (&off)[NT],
-                                            int s0, int s1, int columns, int* acc, int lane, Wait wait) {
-  constexpr int U = NT <= 2 ? 4 : 2;
-  const int i = lane & 3, g = lane >> 2;
-  int d[NT][4];
+// The rows of an item that this lane loads, from its first step on, and the bytes left of them.
+struct Rows {
+  const signed char *a, *b;
+  int left;
+};
+
+// The weights of U steps of 64 bytes on their way.
+template <int kGrid, int U>
+struct Flight {
+  Bytes16<kGrid> a[U], b[U];
+  __device__ __forceinline__ void load(int u, const Rows& r) {
+    load_bytes<kGrid>(a[u], r.a + 64 * u, r.left - 64 * u);
+    load_bytes<kGrid>(b[u], r.b + 64 * u, r.left - 64 * u);
+  }
+};
+
+// Products of 16 weight rows with 8 NT columns of digits (this lane's columns begin at z) over n steps of 64 bytes; the first U
+// steps are in flight on entry, and those of `next` on return.
+template <int NT, int kGrid, int U>
+__device__ __forceinline__ void stream_rows(Flight<kGrid, U>& f, Rows r, const Rows& next, const signed char* const (&z)[NT], int n, int (&d)[NT][4]) {
+  const int sa = 8 * (int)((unsigned long long)r.a & 3ull), sb = 8 * (int)((unsigned long long)r.b & 3ull);
 #pragma unroll
   for (int t = 0; t < NT; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0;
-  uint4 a[U], b[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int pos = (s0 + u) * 64 + 16 * i, end = s0 + u < s1 ? len : 0;
-    a[u] = load_weights<kGrid>(wa, pos, end);
-    b[u] = load_weights<kGrid>(wb, pos, end);
-  }
-  if (!wait()) return;
-  for (int s = s0; s < s1; s += U) {
+  int at = 0;
+#pragma unroll 1
+  for (int s = 0; s < n; s += U, at += 64 * U) {
+    constexpr int A = NT == 1 ? 4 : (NT == 2 ? 2 : 1);  // steps whose digits are loaded together
+    uint4 q[A][NT];
+    if (s + U < n) { r.a += 64 * U; r.b += 64 * U; r.left -= 64 * U; }
+    else r = next;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (s + u < s1) {
+      if (u % A == 0) {
+#pragma unroll
+        for (int v = 0; v < A; ++v)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            if (s + u + v < n) q[v][t] = *reinterpret_cast<const uint4*>(z[t] + at + 64 * (u + v));
+      }
+      if (s + u < n) {
+        const uint4 x = whole_bytes<kGrid>(f.a[u], sa), y = whole_bytes<kGrid>(f.b[u], sb);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          const uint4 z = *reinterpret_cast<const uint4*>(cols + off[t] + (size_t)(s + u) * 64);
-          mma_16x8x32(d[t], a[u].x, b[u].x, a[u].y, b[u].y, z.x, z.y);
-          mma_16x8x32(d[t], a[u].z, b[u].z, a[u].w, b[u].w, z.z, z.w);
+          const uint4 v = q[u % A][t];
+          mma_16x8x32(d[t], x.x, y.x, x.y, y.y, v.x, v.y);
+          mma_16x8x32(d[t], x.z, y.z, x.w, y.w, v.z, v.w);
         }
       }
-      const int n = s + u + U, pos = n * 64 + 16 * i, end = n < s1 ? len : 0;
-      a[u] = load_weights<kGrid>(wa, pos, end);
-      b[u] = load_weights<kGrid>(wb, pos, end);
+      f.load(u, r);
     }
   }
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int col = 8 * t + 2 * i + (j & 1);
-      if (col < columns) atomicAdd(acc + col * kAccPitch + g + 8 * (j >> 1), d[t][j]);
-    }
 }
 
-// The digits of one row of inner activations, by a warp.
+__device__ __forceinline__ float4 load_h4(const MoeParams& p, int row, int i) {
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (i < p.I) v = __ldcg(reinterpret_cast<const float4*>(p.h + (size_t)row * p.h_pitch + i));
+  if (i + 1 >= p.I) v.y = 0.0f;
+  if (i + 2 >= p.I) v.z = 0.0f;
+  if (i + 3 >= p.I) v.w = 0.0f;
+  return v;
+}
+// The digits of one row of inner activations, by a warp; zero behind the row's end.
 __device__ __forceinline__ void make_digits(const MoeParams& p, int row, int lane) {
-  const float* h = p.h + (size_t)row * p.I;
+  constexpr int kHeld = 8;  // values kept between the maximum and the digits: rows up to 1024 are read once
+  float4 held[kHeld];
   unsigned m = 0;
-  for (int i = lane; i < p.I; i += 32) m = max(m, abs_word(__ldcg(h + i)));
-  m = warp_max(m);
-  const DigitScale s = digit_scale(m);
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) held[j] = load_h4(p, row, 4 * lane + 128 * j);
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) m = max(m, max(max(abs_word(held[j].x), abs_word(held[j].y)), max(abs_word(held[j].z), abs_word(held[j].w))));
+  for (int i = 4 * lane + 128 * kHeld; i < p.I; i += 128) {
+    const float4 v = load_h4(p, row, i);
+    m = max(m, max(max(abs_word(v.x), abs_word(v.y)), max(abs_word(v.z), abs_word(v.w))));
+  }
+  const DigitScale s = digit_scale(warp_max(m));
   if (lane == 0) p.h_factor[row] = s.factor;
   signed char* out = p.hd + (size_t)row * 3 * p.h_pitch;
-  for (int i = 4 * lane; i < p.h_pitch; i += 128) {
-    float4 v;
-    v.x = i < p.I ? __ldcg(h + i) : 0.0f;
-    v.y = i + 1 < p.I ? __ldcg(h + i + 1) : 0.0f;
-    v.z = i + 2 < p.I ? __ldcg(h + i + 2) : 0.0f;
-    v.w = i + 3 < p.I ? __ldcg(h + i + 3) : 0.0f;
+  auto put = [&](const float4& v, int i) {
     unsigned a, b, c;
     digits_4(v, s, a, b, c);
     *reinterpret_cast<unsigned*>(out + i) = a;
     *reinterpret_cast<unsigned*>(out + p.h_pitch + i) = b;
     *reinterpret_cast<unsigned*>(out + 2 * (size_t)p.h_pitch + i) = c;
+  };
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (4 * lane + 128 * j < p.h_pitch) put(held[j], 4 * lane + 128 * j);
+  for (int i = 4 * lane + 128 * kHeld; i < p.h_pitch; i += 128) put(load_h4(p, row, i), i);
+}
+
+// All items of a phase, drawn by groups of ks warps.  S says what an item is: rows() its weights, columns() its digits,
+// finish() takes the accumulators acc[column][16], complete() counts the item as done.
+template <int NT, int kGrid, typename S>
+__device__ __forceinline__ void run_phase(const S& job, int items, int steps, int ks, unsigned* ticket, const int* s_first, int* s_next, int* acc_all, int area,
+                                          int lane, int warp) {
+  constexpr int U = kGrid == 1 ? 4 : (NT > 2 ? 6 : 8);
+  const int group = warp / ks, part = warp - group * ks, gtid = part * 32 + lane, threads = 32 * ks;
+  const int per = (steps + ks - 1) / ks, s0 = min(steps, part * per), n = min(steps, s0 + per) - s0;
+  int* const acc = acc_all + group * area;
+  auto meet = [&] {
+    if (ks == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
+  };
+  int cur = s_first[group], nxt = 0;
+  if (gtid == 0) s_next[group] = (int)atomicAdd(ticket, 1u);
+  Rows rows = job.rows(cur, items, s0, n, lane), after;
+  Flight<kGrid, U> f;
+#pragma unroll
+  for (int u = 0; u < U; ++u) f.load(u, rows);
+  if (ks > 1) for (int i = gtid; i < area; i += threads) acc[i] = 0;
+  meet();
+  while (cur < items) {
+    nxt = s_next[group];
+    meet();
+    unsigned drawn = 0;  // (waited for behind the stream)
+    if (gtid == 0) drawn = atomicAdd(ticket, 1u);
+    after = job.rows(nxt, items, s0, n, lane);
+    const int count = job.count(cur);
+    auto go = [&](auto nt) {
+      constexpr int N = decltype(nt)::value;
+      const signed char* z[N];
+      job.columns(cur, count, s0, lane, z);
+      int d[N][4];
+      stream_rows<N, kGrid, U>(f, rows, after, z, n, d);
+      const int i = lane & 3, g = lane >> 2;
+#pragma unroll
+      for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int col = 8 * t + 2 * i + (j & 1);
+          if (col < 3 * count) {
+            int* q = acc + col * kAccPitch + g + 8 * (j >> 1);
+            if (ks == 1) *q = d[t][j];
+            else atomicAdd(q, d[t][j]);
+          }
+        }
+    };
+    if (NT <= 2 || count <= 5) go(std::integral_constant<int, (NT < 2 ? NT : 2)>{});
+    else go(std::integral_constant<int, NT>{});
+    if (gtid == 0) s_next[group] = (int)drawn;
+    meet();
+    job.finish(cur, count, acc, gtid, threads);
+    meet();
+    if (ks > 1) for (int i = gtid; i < 3 * count * kAccPitch; i += threads) acc[i] = 0;
+    if (part == 0) job.complete(cur, lane);
+    rows = after;
+    cur = nxt;
   }
 }
 
-// Shared memory of a block, in bytes: lists of rows, masks by expert, accumulators of either phase.
+// Shared memory of a block: accumulators of its warps, lists of rows.  The logits' keys [T][E] lie over the accumulators until
+// the choice is made.
 struct MoeShared {
-  int rows, acc_ints, chosen, total;
+  int rows, chosen, area, lists_at, total;
   __host__ __device__ MoeShared(int T, int k, int E) {
     rows = T * k;
-    const int one = kMoeWarps * 3 * T * kAccPitch, two = 3 * rows * kAccPitch;  // every warp an item; every row
-    acc_ints = one > two ? one : two;
     chosen = rows < E ? rows : E;
-    total = 4 * (acc_ints + 6 * rows + 16 * rows + 2 * E) + 64;
+    area = 3 * T * kAccPitch;
+    lists_at = 4 * kMoeWarps * area;
+    if (lists_at < 8 * T * E) lists_at = 8 * T * E;
+    total = lists_at + 4 * (7 * rows + 2 * E);
   }
 };
 
-template <int kGridC, int kGridI>
-__global__ void __launch_bounds__(kMoeThreads, 1) moe_experts_kernel(const __grid_constant__ MoeParams p, const int kw) {
+// Phase one: eight inner units of an expert, their gate rows and their up rows.
+struct GateUp {
+  const MoeParams& p;
+  const MoeChoice& ch;
+  unsigned *done, *ready;
+  __device__ __forceinline__ int expert(int item) const { return p.by_unit_blocks(item); }
+  __device__ __forceinline__ int count(int item) const { return __popc(ch.tokens[expert(item)]); }
+  __device__ __forceinline__ Rows rows(int item, int items, int s0, int n, int lane) const {
+    Rows r{p.wgu, p.wgu, 0};
+    if (item >= items) return r;
+    const int a = expert(item), unit = min((item - a * p.unit_blocks) * 8 + (lane >> 2), p.I - 1);
+    const int from = 64 * s0 + 16 * (lane & 3);
+    r.a = p.wgu + ((size_t)ch.expert[a] * 2 * p.I + unit) * p.C + from;
+    r.b = r.a + (size_t)p.I * p.C;
+    r.left = min(p.C, 64 * (s0 + n)) - from;
+    return r;
+  }
+  template <int NT>
+  __device__ __forceinline__ void columns(int item, int count, int s0, int lane, const signed char* (&z)[NT]) const {
+    const int first = ch.first[expert(item)];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int col = min(8 * t + (lane >> 2), 3 * count - 1), r = col / 3;
+      z[t] = p.xd + (size_t)(ch.row_token[first + r] * 3 + col - 3 * r) * p.x_pitch + 64 * s0 + 16 * (lane & 3);
+    }
+  }
+  __device__ __forceinline__ void finish(int item, int count, const int* acc, int tid, int threads) const {
+    const int a = expert(item), i0 = (item - a * p.unit_blocks) * 8, first = ch.first[a];
+    for (int o = tid; o < 8 * count; o += threads) {
+      const int r = o >> 3, u = o & 7, i = i0 + u;
+      if (i >= p.I) continue;
+      const int* q = acc + 3 * r * kAccPitch + u;
+      const float f = p.x_factor[ch.row_token[first + r]];
+      const float* s = p.sgu + (size_t)ch.expert[a] * 2 * p.I + i;
+      const float g = __fmul_rn(__fmul_rn(digits_sum(q[0], q[kAccPitch], q[2 * kAccPitch]), f), s[0]);
+      const float v = __fmul_rn(__fmul_rn(digits_sum(q[8], q[kAccPitch + 8], q[2 * kAccPitch + 8]), f), s[p.I]);
+      p.h[(size_t)(first + r) * p.h_pitch + i] = __fmul_rn(__fdiv_rn(g, __fadd_rn(1.0f, expf(-g))), v);
+    }
+  }
+  __device__ __forceinline__ void complete(int item, int lane) const {
+    const int a = expert(item);
+    unsigned old = 0;
+    if (lane == 0) { __threadfence(); old = atomicAdd(&done[a], 1u); __threadfence(); }
+    if (__shfl_sync(0xffffffffu, old, 0) + 1u != (unsigned)p.unit_blocks) return;
+    for (int r = 0, n = __popc(ch.tokens[a]); r < n; ++r) make_digits(p, ch.first[a] + r, lane);
+    __syncwarp();
+    if (lane == 0) { __threadfence(); store_release(&ready[a], 1u); }
+  }
+};
+
+// Phase two: sixteen output channels of an expert, expert by expert in the order in which phase one completes them.
+struct Down {
+  const MoeParams& p;
+  const MoeChoice& ch;
+  unsigned *ready, *tile_done;
+  unsigned char* known;
+  int* gave_up;
+  int active;
+  __device__ __forceinline__ int expert(int item) const { return p.by_tiles(item); }
+  __device__ __forceinline__ int tile(int item) const { return item - p.by_tiles(item) * p.tiles; }
+  __device__ __forceinline__ int count(int item) const { return __popc(ch.tokens[expert(item)]); }
+  __device__ __forceinline__ Rows rows(int item, int items, int s0, int n, int lane) const {
+    Rows r{p.wd, p.wd, 0};
+    if (item >= items) return r;
+    const int a = expert(item), t = item - a * p.tiles, c = 16 * t + (lane >> 2), from = 64 * s0 + 16 * (lane & 3);
+    const signed char* w = p.wd + (size_t)ch.expert[a] * p.C * p.I + from;
+    r.a = w + (size_t)min(c, p.C - 1) * p.I;
+    r.b = w + (size_t)min(c + 8, p.C - 1) * p.I;
+    r.left = min(p.I, 64 * (s0 + n)) - from;
+    return r;
+  }
+  template <int NT>
+  __device__ __forceinline__ void columns(int item, int count, int s0, int lane, const signed char* (&z)[NT]) const {
+    const int a = expert(item);
+    // (lines of digits belong to one expert: none can be in L1 from before its flag)
+    if (!__any_sync(0xffffffffu, *reinterpret_cast<volatile unsigned char*>(known + a)) && wait_raised(&ready[a], gave_up, p.status))
+      *reinterpret_cast<volatile unsigned char*>(known + a) = 1;
+    __threadfence_block();
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int col = min(8 * t + (lane >> 2), 3 * count - 1);
+      z[t] = p.hd + (size_t)(ch.first[a] * 3 + col) * p.h_pitch + 64 * s0 + 16 * (lane & 3);
+    }
+  }
+  __device__ __forceinline__ void finish(int item, int count, const int* acc, int tid, int threads) const {
+    const int a = expert(item), t = item - a * p.tiles, first = ch.first[a];
+    for (int o = tid; o < 16 * count; o += threads) {
+      const int r = o >> 4, c = 16 * t + (o & 15);
+      if (c >= p.C) continue;
+      const int* q = acc + 3 * r * kAccPitch + (o & 15);
+      const float v = __fmul_rn(digits_sum(q[0], q[kAccPitch], q[2 * kAccPitch]), __ldcg(p.h_factor + first + r));
+      p.part[(size_t)(first + r) * p.C + c] = __fmul_rn(ch.prob[first + r], __fmul_rn(v, p.sd[(size_t)ch.expert[a] * p.C + c]));
+    }
+  }
+  __device__ __forceinline__ void complete(int item, int lane) const {
+    const int t = tile(item);
+    unsigned old = 0;
+    if (lane == 0) { __threadfence(); old = atomicAdd(&tile_done[t], 1u); __threadfence(); }
+    if (__shfl_sync(0xffffffffu, old, 0) + 1u != (unsigned)active) return;
+    const int c = 16 * t + (lane & 15);
+    if (c >= p.C) return;
+    for (int token = lane >> 4; token < p.T; token += 2) {
+      const int* rows = ch.row_of + token * p.k;
+      float y = 0.0f;
+#pragma unroll 8
+      for (int j = 0; j < p.k; ++j) y = __fadd_rn(y, __ldcg(p.part + (size_t)rows[j] * p.C + c));
+      const long long at = (long long)token * p.ldy + c;
+      if (p.x_type == Q8_F32) static_cast<float*>(p.y)[at] = y;
+      else if (p.x_type == Q8_F16) static_cast<__half*>(p.y)[at] = __float2half_rn(y);
+      else static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(y);
+    }
+  }
+};
+
+template <int NT, int kGrid>
+__global__ void __launch_bounds__(kMoeThreads, 1) moe_experts_kernel(const __grid_constant__ MoeParams p) {
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ int s_active, s_ticket[2], s_last[kMoeWarps], gave_up;
+  __shared__ int s_active, s_first[2][kMoeWarps], s_next[kMoeWarps], gave_up;
   const MoeShared lay(p.T, p.k, p.E);
   int* const acc = reinterpret_cast<int*>(smem);
-  float* const sums = reinterpret_cast<float*>(acc + lay.acc_ints);  // [rows][16]
+  unsigned long long* const keys = reinterpret_cast<unsigned long long*>(smem);  // [T][E], until the choice is made
   MoeChoice ch;
-  ch.expert = reinterpret_cast<int*>(sums + 16 * lay.rows);
+  ch.expert = reinterpret_cast<int*>(smem + lay.lists_at);
   ch.tokens = reinterpret_cast<unsigned*>(ch.expert + lay.rows);
   ch.first = reinterpret_cast<int*>(ch.tokens + lay.rows);
   ch.prob = reinterpret_cast<float*>(ch.first + lay.rows);
   ch.row_of = reinterpret_cast<int*>(ch.prob + lay.rows);
   ch.row_expert = ch.row_of + lay.rows;
-  unsigned* const mask = reinterpret_cast<unsigned*>(ch.row_expert + lay.rows);  // [E] tokens that chose an expert
+  ch.row_token = ch.row_expert + lay.rows;
+  unsigned* const mask = reinterpret_cast<unsigned*>(ch.row_token + lay.rows);  // [E] tokens that chose an expert
   int* const index = reinterpret_cast<int*>(mask + p.E);                          // [E] its place among the chosen
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   for (int e = tid; e < p.E; e += kMoeThreads) mask[e] = 0u;
   if (tid == 0) gave_up = 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  // every group's first items; it draws the second ones later, when all blocks that run have their first
+  if (tid < kMoeWarps / p.ks[0]) s_first[0][tid] = (int)atomicAdd(&p.sync[0], 1u);
+  if (tid < kMoeWarps / p.ks[1]) s_first[1][tid] = (int)atomicAdd(&p.sync[1], 1u);
+  for (int i = tid; i < p.T * p.E; i += kMoeThreads) keys[i] = order_key(__ldcg(p.logits + i));
   __syncthreads();
   // ---- choice: a warp per token
-  int mine = -1;        // lane j: the j-th chosen expert
-  float weight = 0.0f;  // ... its probability
-  if (warp < p.T) {
-    const double* l = p.logits + (size_t)warp * p.E;
-    double best0 = 0.0, v_mine = 0.0;
-    unsigned long long taken = 0ull;  // bit q: expert lane + 32 q (up to 1024 experts: 32 bits)
+  const int per_warp = (p.T + kMoeWarps - 1) / kMoeWarps;  // 1 or 2
+  int mine[2] = {-1, -1};           // lane j: the j-th chosen expert
+  float weight[2] = {0.0f, 0.0f};   // ... its probability
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const int t = warp + w * kMoeWarps;
+    if (w >= per_warp || t >= p.T) break;
+    const unsigned long long* l = keys + (size_t)t * p.E;
+    unsigned long long key0 = 0ull, key_mine = 0ull;
+    unsigned taken = 0u;  // bit q: expert lane + 32 q
     for (int j = 0; j < p.k; ++j) {
       unsigned long long key = 0ull;
       int at = 0x7fffffff;
       for (int q = 0, e = lane; e < p.E; ++q, e += 32) {
-        if (taken >> q & 1ull) continue;
-        const unsigned long long o = order_key(__ldcg(l + e));
+        if (taken >> q & 1u) continue;
+        const unsigned long long o = l[e];
         if (at == 0x7fffffff || o > key) { key = o; at = e; }
       }
       // among lanes that have a candidate, the largest key, then the lowest expert
-      const unsigned have = at != 0x7fffffff;
+      const bool have = at != 0x7fffffff;
       const unsigned hi = have ? (unsigned)(key >> 32) : 0u;
       const unsigned top_hi = __reduce_max_sync(0xffffffffu, hi);
       const bool in = have && hi == top_hi;
       const unsigned top_lo = __reduce_max_sync(0xffffffffu, in ? (unsigned)key : 0u);
       const int e = (int)__reduce_min_sync(0xffffffffu, in && (unsigned)key == top_lo ? (unsigned)at : 0x7fffffffu);
-      if ((e & 31) == lane) taken |= 1ull << (e >> 5);
-      const double v = __ldcg(l + e);
-      if (j == 0) best0 = v;
-      if (lane == j) { mine = e; v_mine = v; }
+      if ((e & 31) == lane) taken |= 1u << (e >> 5);
+      const unsigned long long top = (unsigned long long)top_hi << 32 | top_lo;
+      if (j == 0) key0 = top;
+      if (lane == j) { mine[w] = e; key_mine = top; }
     }
+    const double best = key_value(key0);
     float total = 0.0f;
-    const float ex = lane < p.k ? expf((float)(v_mine - best0)) : 0.0f;
+    const float ex = lane < p.k ? expf((float)(key_value(key_mine) - best)) : 0.0f;
     if (p.renormalize) total = ex;
-    else for (int e = lane; e < p.E; e += 32) total += expf((float)(__ldcg(l + e) - best0));
+    else for (int e = lane; e < p.E; e += 32) total += expf((float)(key_value(l[e]) - best));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    weight = __fdiv_rn(ex, total);
+    weight[w] = __fdiv_rn(ex, total);
     if (lane < p.k) {
-      atomicOr(&mask[mine], 1u << warp);
+      atomicOr(&mask[mine[w]], 1u << t);
       if (blockIdx.x == 0) {
-        if (p.ids) p.ids[warp * p.k + lane] = mine;
-        if (p.probs) p.probs[warp * p.k + lane] = weight;
+        if (p.ids) p.ids[t * p.k + lane] = mine[w];
+        if (p.probs) p.probs[t * p.k + lane] = weight[w];
       }
     }
   }
@@ -428,138 +669,35 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_experts_kernel(const __gri
     }
     if (lane == 0) s_active = n;
   }
-  if (tid == 32) s_ticket[0] = (int)atomicAdd(&p.sync[0], 1u);
   __syncthreads();
-  if (warp < p.T && lane < p.k) {
-    const int at = index[mine], row = ch.first[at] + __popc(ch.tokens[at] & ((1u << warp) - 1u));
-    int place = 0;
-    for (int j = 0; j < p.k; ++j) place += __shfl_sync((p.k == 32 ? 0xffffffffu : (1u << p.k) - 1u), mine, j) < mine;
-    ch.prob[row] = weight;
-    ch.row_of[warp * p.k + place] = row;
-    ch.row_expert[row] = mine;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const int t = warp + w * kMoeWarps;
+    if (w < per_warp && t < p.T && lane < p.k) {
+      const int at = index[mine[w]], row = ch.first[at] + __popc(ch.tokens[at] & ((1u << t) - 1u));
+      int place = 0;
+      for (int j = 0; j < p.k; ++j) place += __shfl_sync(p.k == 32 ? 0xffffffffu : (1u << p.k) - 1u, mine[w], j) < mine[w];
+      ch.prob[row] = weight[w];
+      ch.row_of[t * p.k + place] = row;
+      ch.row_expert[row] = mine[w];
+      ch.row_token[row] = t;
+    }
   }
   const int active = s_active;
   unsigned* const done = p.sync + 2;
   unsigned* const ready = done + lay.chosen;
+  unsigned char* const known = reinterpret_cast<unsigned char*>(mask);  // (masks are in ch.tokens by now) experts seen ready
 
-  // ---- phase one: kw warps an item
-  const int groups = kMoeWarps / kw, group = warp / kw, part = warp - group * kw;
-  const int items = active * p.unit_blocks, bundles = (items + groups - 1) / groups;
-  const int steps = (p.C + 63) >> 6, per = (steps + kw - 1) / kw;
-  int* const my_acc = acc + group * 3 * p.T * kAccPitch;
-  int parity = 0;
-  for (;;) {
-    const int bundle = s_ticket[parity];
-    if (bundle >= bundles) break;
-    const int item = bundle * groups + group;
-    const bool live = item < items;
-    const int a = live ? item / p.unit_blocks : 0, i0 = (item - a * p.unit_blocks) * 8;
-    const int e = ch.expert[a], count = __popc(ch.tokens[a]);
-    for (int i = tid; i < groups * 3 * p.T * kAccPitch; i += kMoeThreads) acc[i] = 0;
-    __syncthreads();
-    unsigned next = 0;
-    if (tid == 0) next = atomicAdd(&p.sync[0], 1u);
-    if (live) {
-      const int s0 = part * per, s1 = min(steps, s0 + per);
-      const int unit = min(i0 + (lane >> 2), p.I - 1);
-      const signed char* wa = p.wgu + ((size_t)e * 2 * p.I + unit) * p.C;
-      const signed char* wb = wa + (size_t)p.I * p.C;
-      auto go = [&](auto nt) {
-        constexpr int NT = decltype(nt)::value;
-        unsigned off[NT];
-        column_offsets<NT>(ch.tokens[a], count, 0, p.x_pitch, false, lane, off);
-        stream_rows<NT, kGridC>(wa, wb, p.C, p.xd, off, s0, s1, 3 * count, my_acc, lane, [] { return true; });
-      };
-      if (s0 < s1) {
-        if (count <= 2) go(std::integral_constant<int, 1>{});
-        else if (count <= 5) go(std::integral_constant<int, 2>{});
-        else go(std::integral_constant<int, 6>{});
-      }
-    }
-    __syncthreads();
-    if (live) {
-      for (int o = part * 32 + lane; o < 8 * count; o += 32 * kw) {
-        const int r = o >> 3, u = o & 7, i = i0 + u;
-        if (i >= p.I) continue;
-        const int* q = my_acc + 3 * r * kAccPitch + u;
-        const float f = p.x_factor[__fns(ch.tokens[a], 0, r + 1)];
-        const size_t at = (size_t)e * 2 * p.I + i;
-        const float g = __fmul_rn(__fmul_rn(digits_sum(q[0], q[kAccPitch], q[2 * kAccPitch]), f), p.sgu[at]);
-        const float v = __fmul_rn(__fmul_rn(digits_sum(q[8], q[kAccPitch + 8], q[2 * kAccPitch + 8]), f), p.sgu[at + p.I]);
-        p.h[(size_t)(ch.first[a] + r) * p.I + i] = __fmul_rn(__fdiv_rn(g, __fadd_rn(1.0f, expf(-g))), v);
-      }
-    }
-    if (tid == 0) s_ticket[parity ^ 1] = (int)next;
-    __syncthreads();
-    if (part == 0 && lane == 0) {
-      int last = 0;
-      if (live) {
-        __threadfence();
-        last = atomicAdd(&done[a], 1u) == (unsigned)p.unit_blocks - 1u;
-        __threadfence();
-      }
-      s_last[group] = last;
-    }
-    __syncthreads();
-    for (int q = 0; q < groups; ++q) {
-      if (!s_last[q]) continue;  // the same for all threads
-      const int qa = (bundle * groups + q) / p.unit_blocks;
-      if (warp < __popc(ch.tokens[qa])) make_digits(p, ch.first[qa] + warp, lane);
-      __syncthreads();
-      if (tid == 0) { __threadfence(); store_release(&ready[qa], 1u); }
-    }
-    parity ^= 1;
-  }
-
-  // ---- phase two: sixteen output channels, all chosen experts
-  const int hsteps = (p.I + 63) >> 6;
-  int kd = 1;  // warps an expert
-  while (2 * kd * active <= kMoeWarps && 4 * kd <= hsteps) kd *= 2;
-  const int hper = (hsteps + kd - 1) / kd, tasks = active * kd, rows = p.T * p.k;
   __syncthreads();
-  for (;;) {
-    if (tid == 0) s_ticket[0] = (int)atomicAdd(&p.sync[1], 1u);
-    for (int i = tid; i < 3 * rows * kAccPitch; i += kMoeThreads) acc[i] = 0;
-    __syncthreads();
-    const int tile = s_ticket[0];
-    if (tile >= p.tiles) break;
-    const int c0 = tile * 16;
-    for (int task = warp; task < tasks; task += kMoeWarps) {
-      const int a = task / kd, s0 = (task - a * kd) * hper, s1 = min(hsteps, s0 + hper);
-      if (s0 >= s1) continue;
-      const int e = ch.expert[a], count = __popc(ch.tokens[a]);
-      const signed char* wa = p.wd + ((size_t)e * p.C + min(c0 + (lane >> 2), p.C - 1)) * p.I;
-      const signed char* wb = p.wd + ((size_t)e * p.C + min(c0 + (lane >> 2) + 8, p.C - 1)) * p.I;
-      auto go = [&](auto nt) {
-        constexpr int NT = decltype(nt)::value;
-        unsigned off[NT];
-        column_offsets<NT>(0u, count, ch.first[a], p.h_pitch, true, lane, off);
-        stream_rows<NT, kGridI>(wa, wb, p.I, p.hd, off, s0, s1, 3 * count, acc + 3 * ch.first[a] * kAccPitch, lane,
-                                [&] { return wait_raised(&ready[a], &gave_up, p.status); });
-      };
-      if (count <= 2) go(std::integral_constant<int, 1>{});
-      else if (count <= 5) go(std::integral_constant<int, 2>{});
-      else go(std::integral_constant<int, 6>{});
-    }
-    __syncthreads();
-    for (int o = tid; o < 16 * rows; o += kMoeThreads) {
-      const int r = o >> 4, c = o & 15;
-      const int* q = acc + 3 * r * kAccPitch + c;
-      const float s = p.sd[(size_t)ch.row_expert[r] * p.C + min(c0 + c, p.C - 1)];
-      sums[o] = __fmul_rn(ch.prob[r], __fmul_rn(__fmul_rn(digits_sum(q[0], q[kAccPitch], q[2 * kAccPitch]), __ldcg(p.h_factor + r)), s));
-    }
-    __syncthreads();
-    for (int o = tid; o < 16 * p.T; o += kMoeThreads) {
-      const int t = o >> 4, c = o & 15;
-      if (c0 + c >= p.C) continue;
-      float y = 0.0f;
-      for (int j = 0; j < p.k; ++j) y = __fadd_rn(y, sums[16 * ch.row_of[t * p.k + j] + c]);
-      const long long at = (long long)t * p.ldy + c0 + c;
-      if (p.x_type == Q8_F32) static_cast<float*>(p.y)[at] = y;
-      else if (p.x_type == Q8_F16) static_cast<__half*>(p.y)[at] = __float2half_rn(y);
-      else static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(y);
-    }
-    __syncthreads();
+  for (int e = tid; e < active; e += kMoeThreads) known[e] = 0;
+  {
+    const GateUp job{p, ch, done, ready};
+    run_phase<NT, kGrid>(job, active * p.unit_blocks, p.steps, p.ks[0], &p.sync[0], s_first[0], s_next, acc, lay.area, lane, warp);
+  }
+  __syncthreads();
+  {
+    const Down job{p, ch, ready, ready + lay.chosen, known, &gave_up, active};
+    run_phase<NT, kGrid>(job, active * p.tiles, (p.I + 63) >> 6, p.ks[1], &p.sync[1], s_first[1], s_next, acc, lay.area, lane, warp);
   }
 }
 
@@ -577,38 +715,62 @@ int validate_moe(const q8_moe_desc* d) {
   return Q8_OK;
 }
 
+Divide make_divide(int d) {
+  Divide f{0u, 0u};
+  while ((1ull << f.l) < (unsigned long long)d) ++f.l;
+  f.m = (unsigned)(((1ull << 32) * ((1ull << f.l) - (unsigned long long)d)) / (unsigned long long)d + 1ull);
+  return f;
+}
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 int pitch128(int n) { return (n + 127) & ~127; }  // rows of digits end with their lines
 
-// The workspace of up to kMoeGroup tokens; sets the pointers of `p` where there is one.  Returns its size.
+// Tokens of a pass.
+int group_of(const q8_moe_desc& d) {
+  const int most = kMoeRows / d.top_k < kMoeGroup ? kMoeRows / d.top_k : kMoeGroup;
+  return d.T < most ? d.T : most;
+}
+
+// The workspace of a pass; sets the pointers of `p` where there is one.  Returns its size.
 size_t moe_space(const q8_moe_desc& d, char* ws, MoeParams* p) {
-  const size_t T = d.T < kMoeGroup ? d.T : kMoeGroup, rows = T * d.top_k;
+  const size_t T = (size_t)group_of(d), rows = T * d.top_k;
   size_t at = 0;
   auto take = [&](size_t bytes) { char* q = ws + at; at += up256(bytes); return q; };
   p->logits = reinterpret_cast<double*>(take(T * d.E * sizeof(double)));
   p->x_factor = reinterpret_cast<float*>(take(T * 4));
   p->h_factor = reinterpret_cast<float*>(take(rows * 4));
-  p->sync = reinterpret_cast<unsigned*>(take((2 + 2 * rows) * 4));
+  p->sync = reinterpret_cast<unsigned*>(take((2 + 2 * rows + (size_t)(d.C + 15) / 16) * 4));
   p->xd = reinterpret_cast<signed char*>(take(T * 3 * pitch128(d.C)));
   p->hd = reinterpret_cast<signed char*>(take(rows * 3 * pitch128(d.I)));
-  p->h = reinterpret_cast<float*>(take(rows * d.I * 4));
+  p->part = reinterpret_cast<float*>(take(rows * d.C * 4));
+  p->h = reinterpret_cast<float*>(take(rows * pitch128(d.I) * 4));
   return at;
+}
+
+// How many warps share the reduction of an item: the fewest rounds times steps, a round costing about four steps besides.
+int warps_per_item(double items, int steps) {
+  int best = 1;
+  double least = 1e30;
+  for (int ks = 1; ks <= 4; ks *= 2) {
+    const double cost = ceil(items / (sm_count() * (kMoeWarps / ks))) * ((steps + ks - 1) / ks + 4);
+    if (cost < least) { least = cost; best = ks; }
+  }
+  return best;
 }
 
 int row_grid(const void* w, int len) { return aligned16(w) && len % 16 == 0 ? 16 : (aligned_to(w, 8) && len % 8 == 0 ? 8 : 1); }
 
-template <int kGridC, int kGridI>
-int launch_experts(const MoeParams& p, int kw, cudaStream_t s) {
+template <int NT, int kGrid>
+int launch_experts(const MoeParams& p, cudaStream_t s) {
   const int smem = MoeShared(p.T, p.k, p.E).total;
   static std::atomic<bool> set[kMaxDevices];
   const int dev = current_device();
   if (dev < 0 || !set[dev].load(std::memory_order_relaxed)) {
-    const int rc = check_cuda(cudaFuncSetAttribute(moe_experts_kernel<kGridC, kGridI>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024), "moe_experts_kernel");
+    const int rc = check_cuda(cudaFuncSetAttribute(moe_experts_kernel<NT, kGrid>, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024), "moe_experts_kernel");
     if (rc != Q8_OK) return rc;
     if (dev >= 0) set[dev].store(true, std::memory_order_relaxed);
   }
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(sm_count()));
+  cfg.gridDim = dim3((unsigned)sm_count());
   cfg.blockDim = dim3(kMoeThreads);
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = s;
@@ -617,19 +779,20 @@ int launch_experts(const MoeParams& p, int kw, cudaStream_t s) {
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return check_cuda(cudaLaunchKernelEx(&cfg, moe_experts_kernel<kGridC, kGridI>, p, kw), "moe_experts_kernel");
+  return check_cuda(cudaLaunchKernelEx(&cfg, moe_experts_kernel<NT, kGrid>, p), "moe_experts_kernel");
 }
 
-template <int kGridC>
-int launch_experts(const MoeParams& p, int grid_i, int kw, cudaStream_t s) {
-  if (grid_i == 16) return launch_experts<kGridC, 16>(p, kw, s);
-  if (grid_i == 8) return launch_experts<kGridC, 8>(p, kw, s);
-  return launch_experts<kGridC, 1>(p, kw, s);
+// Columns for every token of the pass, in eights: three for up to two tokens, fifteen for up to five.
+template <int kGrid>
+int launch_experts(const MoeParams& p, cudaStream_t s) {
+  if (p.T <= 2) return launch_experts<1, kGrid>(p, s);
+  if (p.T <= 5) return launch_experts<2, kGrid>(p, s);
+  return launch_experts<6, kGrid>(p, s);
 }
 
 int launch_route(const MoeParams& p, cudaStream_t s) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(p.T + (p.T * p.E + 7) / 8));
+  cfg.gridDim = dim3((unsigned)(p.T + p.E));
   cfg.blockDim = dim3(256);
   cfg.stream = s;
   cudaLaunchAttribute at[1];
@@ -678,24 +841,28 @@ int q8_moe(const q8_moe_desc* d, const void* x, const float* router, const int8_
   p.router = router; p.wgu = w_gate_up; p.sgu = s_gate_up; p.wd = w_down; p.sd = s_down;
   p.x_pitch = pitch128(p.C); p.h_pitch = pitch128(p.I);
   p.unit_blocks = (p.I + 7) / 8; p.tiles = (p.C + 15) / 16;
+  p.steps = (p.C + 63) / 64;
+  p.by_unit_blocks = make_divide(p.unit_blocks); p.by_tiles = make_divide(p.tiles);
   p.x_vec = aligned_to(x, 4 * e) && p.ldx % 4 == 0 && p.C % 4 == 0;
   p.r_vec = aligned16(router) && p.C % 4 == 0;
   p.status = status_word_device_ptr();
   if (!p.status) return fail(Q8_ERR_CUDA, "q8_moe: status word not available");
   cudaStream_t s = as_stream(stream);
-  for (int t0 = 0; t0 < d->T; t0 += kMoeGroup) {
-    p.T = d->T - t0 < kMoeGroup ? d->T - t0 : kMoeGroup;
+  const int group = group_of(*d), gc = row_grid(w_gate_up, p.C), gi = row_grid(w_down, p.I), grid = gc < gi ? gc : gi;
+  for (int t0 = 0; t0 < d->T; t0 += group) {
+    p.T = d->T - t0 < group ? d->T - t0 : group;
+    // experts that some token chooses, as many as independent choices give
+    double missed = 1.0;
+    for (int t = 0; t < p.T; ++t) missed *= 1.0 - (double)p.k / p.E;
+    const double chosen = p.E * (1.0 - missed);
+    p.ks[0] = warps_per_item(chosen * p.unit_blocks, p.steps);
+    p.ks[1] = warps_per_item(chosen * p.tiles, (p.I + 63) / 64);
     p.x = static_cast<const char*>(x) + (size_t)t0 * p.ldx * e;
     p.y = static_cast<char*>(y) + (size_t)t0 * p.ldy * e;
     p.ids = ids ? ids + (size_t)t0 * p.k : nullptr;
     p.probs = probs ? probs + (size_t)t0 * p.k : nullptr;
     if ((rc = launch_route(p, s)) != Q8_OK) return rc;
-    const int kw = 2, gi = row_grid(w_down, p.I);
-    switch (row_grid(w_gate_up, p.C)) {
-      case 16: rc = launch_experts<16>(p, gi, kw, s); break;
-      case 8: rc = launch_experts<8>(p, gi, kw, s); break;
-      default: rc = launch_experts<1>(p, gi, kw, s); break;
-    }
+    rc = grid == 16 ? launch_experts<16>(p, s) : (grid == 8 ? launch_experts<8>(p, s) : launch_experts<1>(p, s));
     if (rc != Q8_OK) return rc;
   }
   return Q8_OK;
