@@ -4,19 +4,25 @@
 // everything between two streams of them is latency.  Two kernels:
 //
 //   moe_route_kernel    logits in 64 bits, a warp per (token, expert); the tokens as integer digits, a block per token;
-//   moe_experts_kernel  all the rest.  Every block finds the chosen experts itself.  Then blocks draw work by tickets: first
-//                       items of eight inner units (their eight gate and eight up rows are the sixteen rows of an
-//                       instruction), then items of sixteen output channels over all chosen experts.
+//   moe_experts_kernel  all the rest.  Every block finds the chosen experts itself.  Then warps draw items by tickets: first
+//                       of eight inner units (their eight gate and eight up rows are the sixteen rows of an instruction),
+//                       then of sixteen output channels of an expert.
 //
 // A value of a token is held as a 24-bit integer relative to the row's largest, in three digits to the base 256 of -128 ..
-// 127: the digits are three more "tokens" of an 8-bit product, which the eight columns of mma.sync.m16n8k32 have to spare
-// (T tokens fill 3 T of 8 ceil(3T/8)).  Weights enter the tensor cores as the bytes they are, no conversion; all sums are
+// 127: the digits are columns of an 8-bit product like tokens, four to a token with one left idle, so that the eight columns
+// of mma.sync.m16n8k32 take two tokens.  Weights enter the tensor cores as the bytes they are, no conversion; all sums are
 // exact integers, so neither the split of a reduction over warps nor the order of their additions changes a bit.
 //
-// What phase two reads of phase one: the block that completes an expert's last item turns the expert's inner activations
-// into digits and raises its flag.  A block waits for the flags only with its first down weights already on their way.
-// Blocks that wait hold a ticket of phase two, so that all items of phase one are in the hands of running blocks: progress
-// needs no co-residency.  Waits are bounded all the same.
+// The order of the products inside an instruction is free as long as both operands share it: a lane's 16 contiguous bytes of
+// a weight row are its operands of two instructions as they come.  They reach the lane through a ring of its warp in shared
+// memory (cp.async, each lane copies what it reads), which runs on across items: bytes in flight cost no registers and do
+// not share a scoreboard with the other loads of the loop.  (Loads to registers, eight steps ahead: every wait for a digit
+// also waited for the weights issued before it; 16 tokens, 64 experts 124 us.)
+//
+// What phase two reads of phase one: the largest magnitudes of the rows of inner activations are collected while these are
+// made; behind the last item of phase one, warps draw rows, wait for the items of the row's expert and turn it into digits.
+// A warp waits for an expert's rows only with its first down weights already on their way, and with every item it waits for
+// in the hands of a running warp: progress needs no co-residency.  Waits are bounded all the same.
 #include <atomic>
 #include <cmath>
 #include <type_traits>
@@ -31,8 +37,12 @@ constexpr int kMoeRows = 256;    // ... times top_k, at most
 constexpr int kMoeWarps = 16, kMoeThreads = 32 * kMoeWarps;
 constexpr int kMaxTopK = 32;      // a lane each
 constexpr int kMaxExperts = 1024; // a bit of a lane's word each
-constexpr int kAccPitch = 20;    // ints between two columns of accumulators: lanes of a warp meet no bank twice
+constexpr int kDepth1 = 5;       // steps of 16 x 64 bytes in a warp's ring: 80 KiB of weights on their way to an SM
+constexpr int kDepth2 = 5;       // ... in phase two
+constexpr int kDepth2Odd = 5;    // ... where a step takes 1280 bytes
 constexpr float kDigitMax = 8355711.0f;  // 127 (256^2 + 256 + 1)
+constexpr int kTickets = 6;
+constexpr int kDirectSteps = 32; // tokens times steps up to which the readers of inner activations make their digits themselves
 constexpr unsigned kTimeoutMoe = 32u;
 constexpr unsigned long long kMoeWaitNs = 2000000000ull;
 
@@ -57,14 +67,15 @@ struct MoeParams {
   // workspace
   double* logits;        // [T][E]
   float* x_factor;       // [T]
-  float* h_factor;       // [T k]
-  unsigned* sync;        // two tickets; per chosen expert the finished items, then the flags; finished items per tile
+  unsigned* sync;        // tickets (blocks and items of either phase, rows, tiles); per chosen expert the finished items, then the rows made digits; finished items per
+                         // tile; per row its largest magnitude
   float* part;           // weighted results of the experts [T k][C]
   signed char* xd;       // digits of the tokens [T][3][x_pitch]
   signed char* hd;       // digits of the inner activations [T k][3][h_pitch]
   float* h;              // inner activations [T k][h_pitch]
   int x_pitch, h_pitch;  // multiples of 128
   int unit_blocks, tiles, steps;  // items of an expert in phase one; items of phase two; steps of an item of phase one
+  int direct;                     // see kDirectSteps (until launch: the room it takes, or 0)
   int ks[2];                      // warps that share the reduction of an item, by phase
   Divide by_unit_blocks, by_tiles;
   int x_vec, r_vec;
@@ -135,7 +146,7 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if ((int)blockIdx.x < p.T) {  // digits of a token
     const int t = blockIdx.x;
-    if (t == 0) for (int i = threadIdx.x; i < 2 + 2 * min(p.E, p.T * p.k) + p.tiles; i += 256) p.sync[i] = 0u;
+    if (t == 0) for (int i = threadIdx.x; i < kTickets + 2 * min(p.E, p.T * p.k) + p.tiles + p.T * p.k; i += 256) p.sync[i] = 0u;
     __shared__ unsigned part[8];
     unsigned m = 0;
     if (p.x_vec) {
@@ -236,24 +247,26 @@ struct MoeChoice {
   int* first;           // [rows] ... their first row
   float* prob;          // [rows] by row
   int* row_of;          // [T][k] rows of a token, ascending
-  int* row_expert;      // [rows]
   int* row_token;       // [rows]
+  int* row_at;          // [rows] place of the row's expert among the chosen
 };
 
-__device__ __forceinline__ int load_acquire(const unsigned* p) {
+__device__ __forceinline__ unsigned load_acquire(const unsigned* p) {
   unsigned v;
   asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-  return (int)v;
+  return v;
 }
-__device__ __forceinline__ void store_release(unsigned* p, unsigned v) {
-  asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+// Counts what this warp has written (all its lanes are behind a __syncwarp); nobody waits for the answer.
+__device__ __forceinline__ void add_release(unsigned* p, unsigned v) {
+  __threadfence();
+  asm volatile("red.relaxed.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }
 
-// Whether `*flag` was raised in time.  All lanes of a warp call it.
-__device__ __noinline__ bool wait_raised(const unsigned* flag, volatile int* gave_up, unsigned* status) {
+// Whether `*counter` reached n in time.  All lanes of a warp call it.
+__device__ __noinline__ bool wait_counted(const unsigned* counter, unsigned n, volatile int* gave_up, unsigned* status) {
   unsigned long long t0 = 0;
   for (unsigned spins = 1;; ++spins) {
-    if (__all_sync(0xffffffffu, load_acquire(flag) != 0)) return true;
+    if (__all_sync(0xffffffffu, load_acquire(counter) == n)) return true;
     if ((spins & 255u) == 0) {
       unsigned long long now;
       asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
@@ -268,88 +281,80 @@ __device__ __noinline__ bool wait_raised(const unsigned* flag, volatile int* gav
   }
 }
 
-// Sixteen bytes of a weight row as they are loaded, zero from the row's end on.  kGrid: 16 or 8, the alignment of every row,
-// or 1: rows anywhere, read as aligned words each of which holds a byte of the row.  `left`: bytes of the row from `at` on.
-template <int kGrid>
-struct Bytes16 {
-  unsigned w[kGrid == 1 ? 5 : 4];
-};
-template <int kGrid>
-__device__ __forceinline__ void load_bytes(Bytes16<kGrid>& v, const signed char* at, int left) {
-#pragma unroll
-  for (int k = 0; k < (kGrid == 1 ? 5 : 4); ++k) v.w[k] = 0u;
-  if constexpr (kGrid == 16) {
-    if (left > 0) asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "l"(at));
-  } else if constexpr (kGrid == 8) {
-    if (left > 0) asm volatile("ld.global.nc.v2.u32 {%0, %1}, [%2];" : "=r"(v.w[0]), "=r"(v.w[1]) : "l"(at));
-    if (left > 8) asm volatile("ld.global.nc.v2.u32 {%0, %1}, [%2];" : "=r"(v.w[2]), "=r"(v.w[3]) : "l"(at + 8));
-  } else {
-    const unsigned* w = reinterpret_cast<const unsigned*>((unsigned long long)at & ~3ull);
-    const int m = (int)((unsigned long long)at & 3ull);
-#pragma unroll
-    for (int k = 0; k < 5; ++k)
-      if (4 * k - m < left && (k < 4 || m > 0)) asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v.w[k]) : "l"(w + k));
-  }
-}
-template <int kGrid>
-__device__ __forceinline__ uint4 whole_bytes(const Bytes16<kGrid>& v, int shift) {
-  if constexpr (kGrid != 1) return make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
-  else return make_uint4(__funnelshift_r(v.w[0], v.w[1], shift), __funnelshift_r(v.w[1], v.w[2], shift), __funnelshift_r(v.w[2], v.w[3], shift),
-                         __funnelshift_r(v.w[3], v.w[4], shift));
+__device__ __forceinline__ void copy_async_16(void* shared, const void* global) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(global) : "memory");
 }
 
-// The rows of an item that this lane loads, from its first step on, and the bytes left of them.
+// The rows of an item that this lane copies, from its present step on, and the bytes left of them.
 struct Rows {
   const signed char *a, *b;
   int left;
 };
 
-// The weights of U steps of 64 bytes on their way.
-template <int kGrid, int U>
-struct Flight {
-  Bytes16<kGrid> a[U], b[U];
-  __device__ __forceinline__ void load(int u, const Rows& r) {
-    load_bytes<kGrid>(a[u], r.a + 64 * u, r.left - 64 * u);
-    load_bytes<kGrid>(b[u], r.b + 64 * u, r.left - 64 * u);
+// A warp's ring.  kGrid: 16 or 8, the alignment of every row, or 1: rows anywhere, copied as aligned words each of which holds
+// a byte of the row and put together when they are read.
+template <int kGrid, int kDepth>
+struct Ring {
+  // (depths are chosen so that `room` in MoeShared holds a step of every token's digits, 192 T bytes, within all limits)
+  static constexpr int kStep = kGrid == 1 ? 1280 : 1024, kHalf = kStep / 2, kBytes = kDepth * kStep;
+  const unsigned char* at;  // this lane's bytes of slot 0
+  uint32_t to;
+  int in, out;              // bytes from there to the slots of the next step copied and used
+  int flying;               // steps between them
+  __device__ __forceinline__ void init(const unsigned char* ring, int lane) {
+    at = ring + (kGrid == 1 ? 4 : 16) * lane;
+    to = (uint32_t)__cvta_generic_to_shared(at);
+    in = out = flying = 0;
   }
-};
-
-// Products of 16 weight rows with 8 NT columns of digits (this lane's columns begin at z) over n steps of 64 bytes; the first U
-// steps are in flight on entry, and those of `next` on return.
-template <int NT, int kGrid, int U>
-__device__ __forceinline__ void stream_rows(Flight<kGrid, U>& f, Rows r, const Rows& next, const signed char* const (&z)[NT], int n, int (&d)[NT][4]) {
-  const int sa = 8 * (int)((unsigned long long)r.a & 3ull), sb = 8 * (int)((unsigned long long)r.b & 3ull);
+  template <int kBytes>
+  static __device__ __forceinline__ void copy(uint32_t dst, const void* src, bool live) {
+    const int n = live ? kBytes : 0;  // none: zeros
+    if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(kBytes), "r"(n) : "memory");
+  }
+  static __device__ __forceinline__ void copy_row(uint32_t dst, const signed char* row, int left) {
+    if constexpr (kGrid == 16) {
+      copy<16>(dst, row, left > 0);
+    } else if constexpr (kGrid == 8) {
+      copy<8>(dst, row, left > 0);
+      copy<8>(dst + 8, row + 8, left > 8);
+    } else {
+      const int m = (int)((unsigned long long)row & 3ull);
 #pragma unroll
-  for (int t = 0; t < NT; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0;
-  int at = 0;
-#pragma unroll 1
-  for (int s = 0; s < n; s += U, at += 64 * U) {
-    constexpr int A = NT == 1 ? 4 : (NT == 2 ? 2 : 1);  // steps whose digits are loaded together
-    uint4 q[A][NT];
-    if (s + U < n) { r.a += 64 * U; r.b += 64 * U; r.left -= 64 * U; }
-    else r = next;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (u % A == 0) {
-#pragma unroll
-        for (int v = 0; v < A; ++v)
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-            if (s + u + v < n) q[v][t] = *reinterpret_cast<const uint4*>(z[t] + at + 64 * (u + v));
-      }
-      if (s + u < n) {
-        const uint4 x = whole_bytes<kGrid>(f.a[u], sa), y = whole_bytes<kGrid>(f.b[u], sb);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const uint4 v = q[u % A][t];
-          mma_16x8x32(d[t], x.x, y.x, x.y, y.y, v.x, v.y);
-          mma_16x8x32(d[t], x.z, y.z, x.w, y.w, v.z, v.w);
-        }
-      }
-      f.load(u, r);
+      for (int k = 0; k < 5; ++k) copy<4>(dst + 128 * k, row - m + 4 * k, 4 * k - m < left && (k < 4 || m > 0));
     }
   }
-}
+  static __device__ __forceinline__ uint4 read_row(const unsigned char* src, const signed char* row) {
+    if constexpr (kGrid != 1) {
+      return *reinterpret_cast<const uint4*>(src);
+    } else {
+      const int m = 8 * (int)((unsigned long long)row & 3ull);
+      unsigned u[5];
+#pragma unroll
+      for (int k = 0; k < 5; ++k) u[k] = *reinterpret_cast<const unsigned*>(src + 128 * k);
+      return make_uint4(__funnelshift_r(u[0], u[1], m), __funnelshift_r(u[1], u[2], m), __funnelshift_r(u[2], u[3], m), __funnelshift_r(u[3], u[4], m));
+    }
+  }
+  __device__ __forceinline__ void put(Rows& r) {
+    copy_row(to + in, r.a, r.left);
+    copy_row(to + in + kHalf, r.b, r.left);
+    r.a += 64;
+    r.b += 64;
+    r.left -= 64;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    in = in == (kDepth - 1) * kStep ? 0 : in + kStep;
+    ++flying;
+  }
+  __device__ __forceinline__ void get(const Rows& r, uint4& a, uint4& b) {
+    // a group for each step: with a full ring the oldest is done when all but the others are
+    if (flying == kDepth) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+    --flying;
+    a = read_row(at + out, r.a);
+    b = read_row(at + out + kHalf, r.b);
+    out = out == (kDepth - 1) * kStep ? 0 : out + kStep;
+  }
+};
 
 __device__ __forceinline__ float4 load_h4(const MoeParams& p, int row, int i) {
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -360,105 +365,174 @@ __device__ __forceinline__ float4 load_h4(const MoeParams& p, int row, int i) {
   return v;
 }
 // The digits of one row of inner activations, by a warp; zero behind the row's end.
-__device__ __forceinline__ void make_digits(const MoeParams& p, int row, int lane) {
-  constexpr int kHeld = 8;  // values kept between the maximum and the digits: rows up to 1024 are read once
-  float4 held[kHeld];
-  unsigned m = 0;
-#pragma unroll
-  for (int j = 0; j < kHeld; ++j) held[j] = load_h4(p, row, 4 * lane + 128 * j);
-#pragma unroll
-  for (int j = 0; j < kHeld; ++j) m = max(m, max(max(abs_word(held[j].x), abs_word(held[j].y)), max(abs_word(held[j].z), abs_word(held[j].w))));
-  for (int i = 4 * lane + 128 * kHeld; i < p.I; i += 128) {
-    const float4 v = load_h4(p, row, i);
-    m = max(m, max(max(abs_word(v.x), abs_word(v.y)), max(abs_word(v.z), abs_word(v.w))));
-  }
-  const DigitScale s = digit_scale(warp_max(m));
-  if (lane == 0) p.h_factor[row] = s.factor;
+__device__ __forceinline__ void make_digits(const MoeParams& p, int row, unsigned largest, int lane) {
+  const DigitScale s = digit_scale(largest);
   signed char* out = p.hd + (size_t)row * 3 * p.h_pitch;
-  auto put = [&](const float4& v, int i) {
+#pragma unroll 8
+  for (int i = 4 * lane; i < p.h_pitch; i += 128) {
     unsigned a, b, c;
-    digits_4(v, s, a, b, c);
+    digits_4(load_h4(p, row, i), s, a, b, c);
     *reinterpret_cast<unsigned*>(out + i) = a;
     *reinterpret_cast<unsigned*>(out + p.h_pitch + i) = b;
     *reinterpret_cast<unsigned*>(out + 2 * (size_t)p.h_pitch + i) = c;
-  };
-#pragma unroll
-  for (int j = 0; j < kHeld; ++j)
-    if (4 * lane + 128 * j < p.h_pitch) put(held[j], 4 * lane + 128 * j);
-  for (int i = 4 * lane + 128 * kHeld; i < p.h_pitch; i += 128) put(load_h4(p, row, i), i);
+  }
 }
 
-// All items of a phase, drawn by groups of ks warps.  S says what an item is: rows() its weights, columns() its digits,
-// finish() takes the accumulators acc[column][16], complete() counts the item as done.
-template <int NT, int kGrid, typename S>
-__device__ __forceinline__ void run_phase(const S& job, int items, int steps, int ks, unsigned* ticket, const int* s_first, int* s_next, int* acc_all, int area,
-                                          int lane, int warp) {
-  constexpr int U = kGrid == 1 ? 4 : (NT > 2 ? 6 : 8);
-  const int group = warp / ks, part = warp - group * ks, gtid = part * 32 + lane, threads = 32 * ks;
+// All items of a phase, by groups of ks warps.  J says what an item is: rows() its weights, scales() the factors of this lane's
+// two rows, columns() its digits, finish() takes the sums of a token with these rows (all lanes call it), complete() counts
+// the item as done.
+//
+// Block b begins with the items b + blocks * group, and draws those behind them by tickets.  b is drawn too, so that blocks
+// that run have the first numbers; a group that finds no more tickets takes over the first items of a block that has not
+// drawn its number.  Whoever then waits for an item knows it in the hands of a running warp.
+template <int NT, int kGrid, int kDepth, typename J>
+__device__ __forceinline__ void run_phase(const J& job, int items, int steps, int ks, unsigned* tickets, int block, int* s_next, int* acc_all,
+                                          const unsigned char* ring_at, int lane, int warp) {
+  const int group = warp / ks, part = warp - group * ks, gtid = part * 32 + lane, threads = 32 * ks, i = lane & 3, g = lane >> 2;
   const int per = (steps + ks - 1) / ks, s0 = min(steps, part * per), n = min(steps, s0 + per) - s0;
-  int* const acc = acc_all + group * area;
+  const int groups = kMoeWarps / ks, blocks = (int)gridDim.x;
+  int* const acc = acc_all + group * (128 * NT) + lane;  // (ks > 1) [4 NT][32]
   auto meet = [&] {
     if (ks == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
   };
-  int cur = s_first[group], nxt = 0;
-  if (gtid == 0) s_next[group] = (int)atomicAdd(ticket, 1u);
-  Rows rows = job.rows(cur, items, s0, n, lane), after;
-  Flight<kGrid, U> f;
+  const bool more = blocks * groups < items;
+  auto draw = [&]() -> int { return more ? blocks * groups + (int)atomicAdd(tickets + 1, 1u) : items; };
+  int taken = block, taken_at = group;  // the block whose first items this group does, and which of them is next
+  int cur = taken < blocks ? taken + blocks * taken_at : items;
+  taken_at = groups;
+  if (gtid == 0) s_next[group] = draw();
+  if (ks > 1 && part == 0) {
 #pragma unroll
-  for (int u = 0; u < U; ++u) f.load(u, rows);
-  if (ks > 1) for (int i = gtid; i < area; i += threads) acc[i] = 0;
-  meet();
-  while (cur < items) {
-    nxt = s_next[group];
+    for (int j = 0; j < 4 * NT; ++j) acc[32 * j] = 0;
+  }
+  Ring<kGrid, kDepth> ring;
+  ring.init(ring_at, lane);
+  for (;;) {
+    Rows r = job.rows(cur, items, s0, n, lane), next = r;
+    int m = cur < items ? n : 0;  // steps of r not copied yet
+#pragma unroll 1
+    for (; m > 0 && ring.flying < kDepth; --m) ring.put(r);
     meet();
-    unsigned drawn = 0;  // (waited for behind the stream)
-    if (gtid == 0) drawn = atomicAdd(ticket, 1u);
-    after = job.rows(nxt, items, s0, n, lane);
-    const int count = job.count(cur);
-    auto go = [&](auto nt) {
-      constexpr int N = decltype(nt)::value;
-      const signed char* z[N];
-      job.columns(cur, count, s0, lane, z);
-      int d[N][4];
-      stream_rows<N, kGrid, U>(f, rows, after, z, n, d);
-      const int i = lane & 3, g = lane >> 2;
+    while (cur < items) {
+      const int nxt = s_next[group];
+      meet();
+      unsigned drawn = (unsigned)items;  // (waited for behind the stream)
+      if (gtid == 0 && nxt < items) drawn = (unsigned)draw();
+      const Rows now = r;  // for the alignment of its rows alone
+      if (nxt < items) next = job.rows(nxt, items, s0, n, lane);
+      bool ahead = false;  // r is the next item's
+      const int count = job.count(cur);
+      const float2 scales = job.scales(cur, g);
+      auto go = [&](auto nt) {
+        constexpr int N = decltype(nt)::value;
+        const signed char* z[N];
+        int d[N][4];
 #pragma unroll
-      for (int t = 0; t < N; ++t)
+        for (int t = 0; t < N; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0;
+        const int chunk = job.prepare(cur, count, n, lane);  // steps whose digits are at hand at a time
+        int c_end = 0;
+#pragma unroll 1
+        for (int s = 0; s < n; ++s) {
+          if (s == c_end) {
+            job.columns(cur, count, s0 + s, min(chunk, n - s), lane, z);
+            c_end += chunk;
+          }
+          uint4 a, b;
+          ring.get(now, a, b);
+#pragma unroll 1
+          do {
+            if (m == 0 && !ahead && nxt < items) { r = next; m = n; ahead = true; }
+            if (m == 0) break;
+            ring.put(r);
+            --m;
+          } while (ring.flying < kDepth);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int col = 8 * t + 2 * i + (j & 1);
-          if (col < 3 * count) {
-            int* q = acc + col * kAccPitch + g + 8 * (j >> 1);
-            if (ks == 1) *q = d[t][j];
-            else atomicAdd(q, d[t][j]);
+          for (int t = 0; t < N; ++t) {
+            const uint4 q = *reinterpret_cast<const uint4*>(z[t]);
+            z[t] += 64;
+            mma_16x8x32(d[t], a.x, b.x, a.y, b.y, q.x, q.y);
+            mma_16x8x32(d[t], a.z, b.z, a.w, b.w, q.z, q.w);
           }
         }
-    };
-    if (NT <= 2 || count <= 5) go(std::integral_constant<int, (NT < 2 ? NT : 2)>{});
-    else go(std::integral_constant<int, NT>{});
-    if (gtid == 0) s_next[group] = (int)drawn;
+        if (gtid == 0) s_next[group] = (int)drawn;
+        if (ks > 1) {
+          if (part > 0) {
+#pragma unroll
+            for (int t = 0; t < N; ++t)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) atomicAdd(acc + 32 * (4 * t + j), d[t][j]);
+          }
+          meet();
+          if (part == 0) {
+#pragma unroll
+            for (int t = 0; t < N; ++t)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) { d[t][j] += acc[32 * (4 * t + j)]; acc[32 * (4 * t + j)] = 0; }
+          }
+        } else {
+          __syncwarp();
+        }
+        if (part == 0) {
+          // lanes of even i hold the first two digits of token 2 t + i / 2, their neighbours the third
+#pragma unroll
+          for (int t = 0; t < N; ++t) {
+            const int third_a = __shfl_xor_sync(0xffffffffu, d[t][0], 1), third_b = __shfl_xor_sync(0xffffffffu, d[t][2], 1);
+            const int token = 2 * t + (i >> 1);
+            job.finish(cur, token, g, !(i & 1) && token < count, digits_sum(d[t][0], d[t][1], third_a), digits_sum(d[t][2], d[t][3], third_b), scales);
+          }
+        }
+      };
+      if (NT <= 2 || count <= 4) go(std::integral_constant<int, (NT < 2 ? NT : 2)>{});
+      else go(std::integral_constant<int, NT>{});
+      if (n == 0 && nxt < items) r = next;
+      if (part == 0) {
+        __syncwarp();
+        job.complete(cur, lane);
+      }
+      cur = nxt;
+    }
+    if (gtid == 0) {
+      int item = items;
+      while (item >= items) {
+        if (taken_at == groups) {
+          taken = (int)atomicAdd(tickets, 1u);
+          if (taken >= blocks) break;
+          taken_at = 0;
+        }
+        item = taken + blocks * taken_at++;
+      }
+      s_next[group] = item < items ? item : items;
+    }
     meet();
-    job.finish(cur, count, acc, gtid, threads);
+    cur = s_next[group];
     meet();
-    if (ks > 1) for (int i = gtid; i < 3 * count * kAccPitch; i += threads) acc[i] = 0;
-    if (part == 0) job.complete(cur, lane);
-    rows = after;
-    cur = nxt;
+    if (cur >= items) return;
+    if (gtid == 0) s_next[group] = items;
   }
 }
 
-// Shared memory of a block: accumulators of its warps, lists of rows.  The logits' keys [T][E] lie over the accumulators until
-// the choice is made.
+// Pitch of rows of digits in shared memory: neighbouring rows in different halves of the banks.
+__host__ __device__ __forceinline__ int staged_pitch(int steps) { return steps * 64 + (steps & 1 ? 0 : 64); }
+
+// Shared memory of a block: lists of rows; partial sums of warps that share items; then the warps' rings and digits, the tokens'
+// in phase one if there is room, a warp's own in phase two.  The logits' keys [T][E] lie over sums and rings until the choice
+// is made.
+constexpr int kMoeSmem = 226 * 1024;
 struct MoeShared {
-  int rows, chosen, area, lists_at, total;
-  __host__ __device__ MoeShared(int T, int k, int E) {
+  int rows, chosen, acc_at, rings_at, digits_at, staged, own_at, room, total;
+  __host__ __device__ MoeShared(int T, int k, int E, int steps, int step_bytes, int nt) {
     rows = T * k;
     chosen = rows < E ? rows : E;
-    area = 3 * T * kAccPitch;
-    lists_at = 4 * kMoeWarps * area;
-    if (lists_at < 8 * T * E) lists_at = 8 * T * E;
-    total = lists_at + 4 * (7 * rows + 2 * E);
+    acc_at = (4 * (7 * rows + 2 * E) + 15) & ~15;
+    rings_at = acc_at + kMoeWarps / 2 * 512 * nt;
+    digits_at = rings_at + kMoeWarps * kDepth1 * step_bytes;
+    if (digits_at < acc_at + 8 * T * E) digits_at = acc_at + 8 * T * E;
+    const int all = 3 * T * staged_pitch(steps);
+    staged = all <= kMoeSmem - digits_at;
+    own_at = rings_at + kMoeWarps * (step_bytes == 1024 ? kDepth2 : kDepth2Odd) * step_bytes;
+    room = ((kMoeSmem - own_at) / kMoeWarps) & ~127;
+    total = kMoeSmem;
   }
 };
 
@@ -466,7 +540,9 @@ struct MoeShared {
 struct GateUp {
   const MoeParams& p;
   const MoeChoice& ch;
-  unsigned *done, *ready;
+  unsigned *done, *largest;
+  const signed char* digits;  // of the tokens, in shared memory or not
+  int pitch;
   __device__ __forceinline__ int expert(int item) const { return p.by_unit_blocks(item); }
   __device__ __forceinline__ int count(int item) const { return __popc(ch.tokens[expert(item)]); }
   __device__ __forceinline__ Rows rows(int item, int items, int s0, int n, int lane) const {
@@ -479,36 +555,37 @@ struct GateUp {
     r.left = min(p.C, 64 * (s0 + n)) - from;
     return r;
   }
+  __device__ __forceinline__ int prepare(int, int, int n, int) const { return n; }
   template <int NT>
-  __device__ __forceinline__ void columns(int item, int count, int s0, int lane, const signed char* (&z)[NT]) const {
-    const int first = ch.first[expert(item)];
+  __device__ __forceinline__ void columns(int item, int count, int s0, int n, int lane, const signed char* (&z)[NT]) const {
+    const int first = ch.first[expert(item)], digit = min((lane >> 2) & 3, 2);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int col = min(8 * t + (lane >> 2), 3 * count - 1), r = col / 3;
-      z[t] = p.xd + (size_t)(ch.row_token[first + r] * 3 + col - 3 * r) * p.x_pitch + 64 * s0 + 16 * (lane & 3);
-    }
+    for (int t = 0; t < NT; ++t)
+      z[t] = digits + (ch.row_token[first + min(2 * t + (lane >> 4), count - 1)] * 3 + digit) * pitch + 64 * s0 + 16 * (lane & 3);
   }
-  __device__ __forceinline__ void finish(int item, int count, const int* acc, int tid, int threads) const {
-    const int a = expert(item), i0 = (item - a * p.unit_blocks) * 8, first = ch.first[a];
-    for (int o = tid; o < 8 * count; o += threads) {
-      const int r = o >> 3, u = o & 7, i = i0 + u;
-      if (i >= p.I) continue;
-      const int* q = acc + 3 * r * kAccPitch + u;
-      const float f = p.x_factor[ch.row_token[first + r]];
-      const float* s = p.sgu + (size_t)ch.expert[a] * 2 * p.I + i;
-      const float g = __fmul_rn(__fmul_rn(digits_sum(q[0], q[kAccPitch], q[2 * kAccPitch]), f), s[0]);
-      const float v = __fmul_rn(__fmul_rn(digits_sum(q[8], q[kAccPitch + 8], q[2 * kAccPitch + 8]), f), s[p.I]);
-      p.h[(size_t)(first + r) * p.h_pitch + i] = __fmul_rn(__fdiv_rn(g, __fadd_rn(1.0f, expf(-g))), v);
+  __device__ __forceinline__ float2 scales(int item, int u) const {
+    const int a = expert(item), i = min((item - a * p.unit_blocks) * 8 + u, p.I - 1);
+    const float* s = p.sgu + (size_t)ch.expert[a] * 2 * p.I + i;
+    return make_float2(__ldg(s), __ldg(s + p.I));
+  }
+  __device__ __forceinline__ void finish(int item, int r, int u, bool live, float gate, float up, float2 s) const {
+    const int a = expert(item), i = (item - a * p.unit_blocks) * 8 + u, row = ch.first[a] + r;
+    unsigned m = 0;
+    if (live && i < p.I) {
+      const float f = p.x_factor[ch.row_token[row]];
+      const float g = __fmul_rn(__fmul_rn(gate, f), s.x), v = __fmul_rn(__fmul_rn(up, f), s.y);
+      const float h = __fmul_rn(__fdiv_rn(g, __fadd_rn(1.0f, expf(-g))), v);
+      p.h[(size_t)row * p.h_pitch + i] = h;
+      m = abs_word(h);
     }
+    // the eight units of a token are eight lanes four apart
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 4));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 8));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 16));
+    if (live && u == 0) atomicMax(&largest[row], m);
   }
   __device__ __forceinline__ void complete(int item, int lane) const {
-    const int a = expert(item);
-    unsigned old = 0;
-    if (lane == 0) { __threadfence(); old = atomicAdd(&done[a], 1u); __threadfence(); }
-    if (__shfl_sync(0xffffffffu, old, 0) + 1u != (unsigned)p.unit_blocks) return;
-    for (int r = 0, n = __popc(ch.tokens[a]); r < n; ++r) make_digits(p, ch.first[a] + r, lane);
-    __syncwarp();
-    if (lane == 0) { __threadfence(); store_release(&ready[a], 1u); }
+    if (lane == 0) add_release(&done[expert(item)], 1u);
   }
 };
 
@@ -516,10 +593,12 @@ struct GateUp {
 struct Down {
   const MoeParams& p;
   const MoeChoice& ch;
-  unsigned *ready, *tile_done;
+  const unsigned *done, *ready, *largest;
+  unsigned* tile_done;
   unsigned char* known;
   int* gave_up;
-  int active;
+  signed char* mine;  // shared memory of this warp for an item's digits
+  int room, active;
   __device__ __forceinline__ int expert(int item) const { return p.by_tiles(item); }
   __device__ __forceinline__ int tile(int item) const { return item - p.by_tiles(item) * p.tiles; }
   __device__ __forceinline__ int count(int item) const { return __popc(ch.tokens[expert(item)]); }
@@ -533,34 +612,76 @@ struct Down {
     r.left = min(p.I, 64 * (s0 + n)) - from;
     return r;
   }
-  template <int NT>
-  __device__ __forceinline__ void columns(int item, int count, int s0, int lane, const signed char* (&z)[NT]) const {
+  __device__ __forceinline__ int prepare(int item, int count, int n, int lane) const {
     const int a = expert(item);
-    // (lines of digits belong to one expert: none can be in L1 from before its flag)
-    if (!__any_sync(0xffffffffu, *reinterpret_cast<volatile unsigned char*>(known + a)) && wait_raised(&ready[a], gave_up, p.status))
+    // (lines of digits belong to one expert: none can be in L1 from before that)
+    if (!__any_sync(0xffffffffu, *reinterpret_cast<volatile unsigned char*>(known + a)) &&
+        (p.direct ? wait_counted(&done[a], (unsigned)p.unit_blocks, gave_up, p.status) : wait_counted(&ready[a], (unsigned)count, gave_up, p.status)))
       *reinterpret_cast<volatile unsigned char*>(known + a) = 1;
     __threadfence_block();
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int col = min(8 * t + (lane >> 2), 3 * count - 1);
-      z[t] = p.hd + (size_t)(ch.first[a] * 3 + col) * p.h_pitch + 64 * s0 + 16 * (lane & 3);
-    }
+    if (3 * count * staged_pitch(n) <= room) return n;
+    return (room / (192 * count) - 1) | 1;  // (the pitch of an odd number of steps is no longer than they are)
   }
-  __device__ __forceinline__ void finish(int item, int count, const int* acc, int tid, int threads) const {
-    const int a = expert(item), t = item - a * p.tiles, first = ch.first[a];
-    for (int o = tid; o < 16 * count; o += threads) {
-      const int r = o >> 4, c = 16 * t + (o & 15);
-      if (c >= p.C) continue;
-      const int* q = acc + 3 * r * kAccPitch + (o & 15);
-      const float v = __fmul_rn(digits_sum(q[0], q[kAccPitch], q[2 * kAccPitch]), __ldcg(p.h_factor + first + r));
-      p.part[(size_t)(first + r) * p.C + c] = __fmul_rn(ch.prob[first + r], __fmul_rn(v, p.sd[(size_t)ch.expert[a] * p.C + c]));
+  // The digits of n steps from s0 on, in the warp's own shared memory.
+  template <int NT>
+  __device__ __forceinline__ void columns(int item, int count, int s0, int n, int lane, const signed char* (&z)[NT]) const {
+    const int first = ch.first[expert(item)], pitch = staged_pitch(n), len = 64 * n, digit = min((lane >> 2) & 3, 2);
+    __syncwarp();  // (all lanes have read what was there)
+    if (p.direct) {
+      for (int r = 0; r < count; ++r) {
+        const DigitScale scale = digit_scale(__ldcg(largest + first + r));
+#pragma unroll 8
+        for (int c = 4 * lane; c < len; c += 128) {
+          unsigned d0, d1, d2;
+          digits_4(load_h4(p, first + r, 64 * s0 + c), scale, d0, d1, d2);
+          signed char* to = mine + 3 * r * pitch + c;
+          *reinterpret_cast<unsigned*>(to) = d0;
+          *reinterpret_cast<unsigned*>(to + pitch) = d1;
+          *reinterpret_cast<unsigned*>(to + 2 * pitch) = d2;
+        }
+      }
+    } else {
+      const signed char* from = p.hd + (size_t)first * 3 * p.h_pitch + 64 * s0;
+      int r = 0, c = 16 * lane;
+      while (c >= len) { c -= len; ++r; }
+      for (;;) {
+        uint4 v[6];
+        int to[6];
+#pragma unroll
+        for (int j = 0; j < 6; ++j) {
+          to[j] = r < 3 * count ? r * pitch + c : -1;
+          if (to[j] >= 0) v[j] = *reinterpret_cast<const uint4*>(from + (size_t)r * p.h_pitch + c);
+          c += 512;
+          while (c >= len) { c -= len; ++r; }
+        }
+#pragma unroll
+        for (int j = 0; j < 6; ++j)
+          if (to[j] >= 0) *reinterpret_cast<uint4*>(mine + to[j]) = v[j];
+        if (__all_sync(0xffffffffu, r >= 3 * count)) break;
+      }
     }
+    __syncwarp();
+#pragma unroll
+    for (int t = 0; t < NT; ++t) z[t] = mine + (min(2 * t + (lane >> 4), count - 1) * 3 + digit) * pitch + 16 * (lane & 3);
+  }
+  __device__ __forceinline__ float2 scales(int item, int u) const {
+    const int a = expert(item), c = 16 * (item - a * p.tiles) + u;
+    const float* s = p.sd + (size_t)ch.expert[a] * p.C;
+    return make_float2(__ldg(s + min(c, p.C - 1)), __ldg(s + min(c + 8, p.C - 1)));
+  }
+  __device__ __forceinline__ void finish(int item, int r, int u, bool live, float low, float high, float2 s) const {
+    if (!live) return;
+    const int a = expert(item), c = 16 * (item - a * p.tiles) + u, row = ch.first[a] + r;
+    const float f = digit_scale(__ldcg(largest + row)).factor, w = ch.prob[row];
+    float* out = p.part + (size_t)row * p.C + c;
+    if (c < p.C) out[0] = __fmul_rn(w, __fmul_rn(__fmul_rn(low, f), s.x));
+    if (c + 8 < p.C) out[8] = __fmul_rn(w, __fmul_rn(__fmul_rn(high, f), s.y));
   }
   __device__ __forceinline__ void complete(int item, int lane) const {
-    const int t = tile(item);
-    unsigned old = 0;
-    if (lane == 0) { __threadfence(); old = atomicAdd(&tile_done[t], 1u); __threadfence(); }
-    if (__shfl_sync(0xffffffffu, old, 0) + 1u != (unsigned)active) return;
+    if (lane == 0) add_release(&tile_done[tile(item)], 1u);
+  }
+  // The results of a tile, by a warp.
+  __device__ __forceinline__ void add_up(int t, int lane) const {
     const int c = 16 * t + (lane & 15);
     if (c >= p.C) return;
     for (int token = lane >> 4; token < p.T; token += 2) {
@@ -579,18 +700,18 @@ struct Down {
 template <int NT, int kGrid>
 __global__ void __launch_bounds__(kMoeThreads, 1) moe_experts_kernel(const __grid_constant__ MoeParams p) {
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ int s_active, s_first[2][kMoeWarps], s_next[kMoeWarps], gave_up;
-  const MoeShared lay(p.T, p.k, p.E);
-  int* const acc = reinterpret_cast<int*>(smem);
-  unsigned long long* const keys = reinterpret_cast<unsigned long long*>(smem);  // [T][E], until the choice is made
+  __shared__ int s_active, s_block[2], s_next[kMoeWarps], gave_up;
+  const MoeShared lay(p.T, p.k, p.E, p.steps, Ring<kGrid, 1>::kStep, NT);
+  int* const acc = reinterpret_cast<int*>(smem + lay.acc_at);
+  unsigned long long* const keys = reinterpret_cast<unsigned long long*>(smem + lay.acc_at);  // [T][E], until the choice is made
   MoeChoice ch;
-  ch.expert = reinterpret_cast<int*>(smem + lay.lists_at);
+  ch.expert = reinterpret_cast<int*>(smem);
   ch.tokens = reinterpret_cast<unsigned*>(ch.expert + lay.rows);
   ch.first = reinterpret_cast<int*>(ch.tokens + lay.rows);
   ch.prob = reinterpret_cast<float*>(ch.first + lay.rows);
   ch.row_of = reinterpret_cast<int*>(ch.prob + lay.rows);
-  ch.row_expert = ch.row_of + lay.rows;
-  ch.row_token = ch.row_expert + lay.rows;
+  ch.row_at = ch.row_of + lay.rows;
+  ch.row_token = ch.row_at + lay.rows;
   unsigned* const mask = reinterpret_cast<unsigned*>(ch.row_token + lay.rows);  // [E] tokens that chose an expert
   int* const index = reinterpret_cast<int*>(mask + p.E);                          // [E] its place among the chosen
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -598,9 +719,17 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_experts_kernel(const __gri
   for (int e = tid; e < p.E; e += kMoeThreads) mask[e] = 0u;
   if (tid == 0) gave_up = 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  // every group's first items; it draws the second ones later, when all blocks that run have their first
-  if (tid < kMoeWarps / p.ks[0]) s_first[0][tid] = (int)atomicAdd(&p.sync[0], 1u);
-  if (tid < kMoeWarps / p.ks[1]) s_first[1][tid] = (int)atomicAdd(&p.sync[1], 1u);
+  signed char* const digits = reinterpret_cast<signed char*>(smem + lay.digits_at);
+  const unsigned char* const ring1 = smem + lay.rings_at + warp * Ring<kGrid, kDepth1>::kBytes;
+  constexpr int kLater = kGrid == 1 ? kDepth2Odd : kDepth2;
+  const unsigned char* const ring2 = smem + lay.rings_at + warp * Ring<kGrid, kLater>::kBytes;
+  signed char* const own = reinterpret_cast<signed char*>(smem + lay.own_at) + warp * lay.room;
+  const int x_staged = staged_pitch(p.steps);
+  if (lay.staged) {  // the tokens' digits, on their way during the choice
+    for (int r = warp; r < 3 * p.T; r += kMoeWarps)
+      for (int c = 16 * lane; c < 64 * p.steps; c += 512) copy_async_16(digits + r * x_staged + c, p.xd + (size_t)r * p.x_pitch + c);
+  }
+  if (tid < 2) s_block[tid] = (int)atomicAdd(&p.sync[2 * tid], 1u);  // this block's number in either phase
   for (int i = tid; i < p.T * p.E; i += kMoeThreads) keys[i] = order_key(__ldcg(p.logits + i));
   __syncthreads();
   // ---- choice: a warp per token
@@ -679,25 +808,46 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_experts_kernel(const __gri
       for (int j = 0; j < p.k; ++j) place += __shfl_sync(p.k == 32 ? 0xffffffffu : (1u << p.k) - 1u, mine[w], j) < mine[w];
       ch.prob[row] = weight[w];
       ch.row_of[t * p.k + place] = row;
-      ch.row_expert[row] = mine[w];
+      ch.row_at[row] = at;
       ch.row_token[row] = t;
     }
   }
   const int active = s_active;
-  unsigned* const done = p.sync + 2;
+  unsigned* const done = p.sync + kTickets;
   unsigned* const ready = done + lay.chosen;
+  unsigned* const tile_done = ready + lay.chosen;
+  unsigned* const largest = tile_done + p.tiles;
   unsigned char* const known = reinterpret_cast<unsigned char*>(mask);  // (masks are in ch.tokens by now) experts seen ready
 
+  asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
   for (int e = tid; e < active; e += kMoeThreads) known[e] = 0;
   {
-    const GateUp job{p, ch, done, ready};
-    run_phase<NT, kGrid>(job, active * p.unit_blocks, p.steps, p.ks[0], &p.sync[0], s_first[0], s_next, acc, lay.area, lane, warp);
+    const GateUp job{p, ch, done, largest, lay.staged ? digits : p.xd, lay.staged ? x_staged : p.x_pitch};
+    run_phase<NT, kGrid, kDepth1>(job, active * p.unit_blocks, p.steps, p.ks[0], &p.sync[0], s_block[0], s_next, acc, ring1, lane, warp);
+  }
+  auto draw = [&](unsigned* ticket) {
+    int v = 0;
+    if (lane == 0) v = (int)atomicAdd(ticket, 1u);
+    return __shfl_sync(0xffffffffu, v, 0);
+  };
+  // ---- the rows of inner activations become digits, a warp a row
+  if (!p.direct) {
+    for (int row; (row = draw(&p.sync[4])) < lay.rows;) {
+      const int a = ch.row_at[row];
+      if (!wait_counted(&done[a], (unsigned)p.unit_blocks, &gave_up, p.status)) break;
+      make_digits(p, row, __ldcg(largest + row), lane);
+      __syncwarp();
+      if (lane == 0) add_release(&ready[a], 1u);
+    }
   }
   __syncthreads();
-  {
-    const Down job{p, ch, ready, ready + lay.chosen, known, &gave_up, active};
-    run_phase<NT, kGrid>(job, active * p.tiles, (p.I + 63) >> 6, p.ks[1], &p.sync[1], s_first[1], s_next, acc, lay.area, lane, warp);
+  const Down job{p, ch, done, ready, largest, tile_done, known, &gave_up, own, lay.room, active};
+  run_phase<NT, kGrid, kLater>(job, active * p.tiles, (p.I + 63) >> 6, p.ks[1], &p.sync[2], s_block[1], s_next, acc, ring2, lane, warp);
+  // ---- the results, a warp a tile of sixteen channels
+  for (int t; (t = draw(&p.sync[5])) < p.tiles;) {
+    if (!wait_counted(&tile_done[t], (unsigned)active, &gave_up, p.status)) break;
+    job.add_up(t, lane);
   }
 }
 
@@ -737,8 +887,7 @@ size_t moe_space(const q8_moe_desc& d, char* ws, MoeParams* p) {
   auto take = [&](size_t bytes) { char* q = ws + at; at += up256(bytes); return q; };
   p->logits = reinterpret_cast<double*>(take(T * d.E * sizeof(double)));
   p->x_factor = reinterpret_cast<float*>(take(T * 4));
-  p->h_factor = reinterpret_cast<float*>(take(rows * 4));
-  p->sync = reinterpret_cast<unsigned*>(take((2 + 2 * rows + (size_t)(d.C + 15) / 16) * 4));
+  p->sync = reinterpret_cast<unsigned*>(take((kTickets + 3 * rows + (size_t)(d.C + 15) / 16) * 4));
   p->xd = reinterpret_cast<signed char*>(take(T * 3 * pitch128(d.C)));
   p->hd = reinterpret_cast<signed char*>(take(rows * 3 * pitch128(d.I)));
   p->part = reinterpret_cast<float*>(take(rows * d.C * 4));
@@ -760,12 +909,14 @@ int warps_per_item(double items, int steps) {
 int row_grid(const void* w, int len) { return aligned16(w) && len % 16 == 0 ? 16 : (aligned_to(w, 8) && len % 8 == 0 ? 8 : 1); }
 
 template <int NT, int kGrid>
-int launch_experts(const MoeParams& p, cudaStream_t s) {
-  const int smem = MoeShared(p.T, p.k, p.E).total;
+int launch_experts(MoeParams p, cudaStream_t s) {
+  const MoeShared lay(p.T, p.k, p.E, p.steps, Ring<kGrid, 1>::kStep, NT);
+  const int smem = lay.total;
+  p.direct = p.direct != 0 && p.direct <= lay.room;
   static std::atomic<bool> set[kMaxDevices];
   const int dev = current_device();
   if (dev < 0 || !set[dev].load(std::memory_order_relaxed)) {
-    const int rc = check_cuda(cudaFuncSetAttribute(moe_experts_kernel<NT, kGrid>, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024), "moe_experts_kernel");
+    const int rc = check_cuda(cudaFuncSetAttribute(moe_experts_kernel<NT, kGrid>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMoeSmem), "moe_experts_kernel");
     if (rc != Q8_OK) return rc;
     if (dev >= 0) set[dev].store(true, std::memory_order_relaxed);
   }
@@ -782,12 +933,12 @@ int launch_experts(const MoeParams& p, cudaStream_t s) {
   return check_cuda(cudaLaunchKernelEx(&cfg, moe_experts_kernel<NT, kGrid>, p), "moe_experts_kernel");
 }
 
-// Columns for every token of the pass, in eights: three for up to two tokens, fifteen for up to five.
+// Columns for every token of the pass, two tokens to eight.
 template <int kGrid>
 int launch_experts(const MoeParams& p, cudaStream_t s) {
   if (p.T <= 2) return launch_experts<1, kGrid>(p, s);
-  if (p.T <= 5) return launch_experts<2, kGrid>(p, s);
-  return launch_experts<6, kGrid>(p, s);
+  if (p.T <= 4) return launch_experts<2, kGrid>(p, s);
+  return launch_experts<8, kGrid>(p, s);
 }
 
 int launch_route(const MoeParams& p, cudaStream_t s) {
@@ -857,6 +1008,8 @@ int q8_moe(const q8_moe_desc* d, const void* x, const float* router, const int8_
     const double chosen = p.E * (1.0 - missed);
     p.ks[0] = warps_per_item(chosen * p.unit_blocks, p.steps);
     p.ks[1] = warps_per_item(chosen * p.tiles, (p.I + 63) / 64);
+    const int run = ((p.I + 63) / 64 + p.ks[1] - 1) / p.ks[1];  // steps of a warp
+    p.direct = p.T * run <= kDirectSteps ? 3 * p.T * staged_pitch(run) : 0;
     p.x = static_cast<const char*>(x) + (size_t)t0 * p.ldx * e;
     p.y = static_cast<char*>(y) + (size_t)t0 * p.ldy * e;
     p.ids = ids ? ids + (size_t)t0 * p.k : nullptr;
