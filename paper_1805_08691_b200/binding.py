@@ -22,7 +22,6 @@ STATUS_NAMES = {0: "Q8_OK", 1: "Q8_ERR_INVALID_ARG", 2: "Q8_ERR_UNSUPPORTED", 3:
                 4: "Q8_ERR_WORKSPACE", 5: "Q8_ERR_CUDA", 6: "Q8_ERR_TIMEOUT", 7: "Q8_ERR_NONFINITE"}
 TORCH_DTYPES = {Q8_U8: torch.uint8, Q8_S8: torch.int8, Q8_S32: torch.int32, Q8_F32: torch.float32, Q8_F16: torch.float16,
                 Q8_BF16: torch.bfloat16}
-_FLOAT_TYPES = {torch.float32: Q8_F32, torch.float16: Q8_F16, torch.bfloat16: Q8_BF16}
 _INT_TYPES = {torch.uint8: Q8_U8, torch.int8: Q8_S8, torch.int32: Q8_S32}
 EXPORTS = ["q8_version", "q8_last_error", "q8_read_status", "q8_calibrate_maxabs", "q8_factor", "q8_requant_scale",
            "q8_bias_factor", "q8_quantize", "q8_quantize_pad_channels", "q8_dequantize", "q8_fold_bn",
@@ -134,7 +133,9 @@ def _load_native():
     module = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(module)
     module.bind(*(C.cast(f, C.c_void_p).value for f in (lib.q8_conv2d, lib.q8_conv2d_then_1x1, lib.q8_calibrate_maxabs, lib.q8_quantize,
-                                                        lib.q8_dequantize, lib.q8_detection_output_workspace_bytes, lib.q8_detection_output)), q8_conv_desc)
+                                                        lib.q8_dequantize, lib.q8_detection_output_workspace_bytes, lib.q8_detection_output,
+                                                        lib.q8_quantize_tokens, lib.q8_dequantize_tokens, lib.q8_linear_workspace_bytes, lib.q8_linear,
+                                                        lib.q8_moe_workspace_bytes, lib.q8_moe)), q8_conv_desc)
     return module
 
 
@@ -473,72 +474,21 @@ def q8_detection_output(sources, priors, variances, classes, background=0, conf_
     return out, counts
 
 
-def _token_rows(t, what, dtypes):
-    """Address, rows, columns and row pitch of a CUDA tensor [..., C] of one of `dtypes` on the current device, whose rows lie a
-    fixed stride apart (a contiguous tensor, or a slice of the last dimension of one)."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in dtypes and t.dim() >= 1):
-        raise TypeError(f"{what}: expected a CUDA tensor of {', '.join(str(d) for d in dtypes)} with at least one dimension")
-    if t.device.index != torch.cuda.current_device():
-        raise TypeError(f"{what}: expected a tensor on the current device")
-    C_ = int(t.shape[-1])
-    rows, pitch = 1, C_
-    if t.numel() == 0:
-        return None, 0, C_, C_
-    if C_ > 1 and t.stride(-1) != 1:
-        raise TypeError(f"{what}: expected unit stride in the last dimension")
-    for i in range(t.dim() - 2, -1, -1):
-        if t.shape[i] != 1:
-            if rows == 1:
-                pitch = t.stride(i)
-            elif t.stride(i) != pitch * rows:
-                raise TypeError(f"{what}: rows are not a fixed stride apart")
-            rows *= int(t.shape[i])
-    if rows > 1 and pitch < C_:
-        raise TypeError(f"{what}: rows overlap")
-    return t.data_ptr(), rows, C_, pitch
-
-
-def _token_vector(t, what, n, dtype=torch.float32):
-    if t is None:
-        return None
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.numel() == n
-            and t.device.index == torch.cuda.current_device()):
-        raise TypeError(f"{what}: expected a contiguous CUDA tensor of {n} {dtype} values on the current device")
-    return t.data_ptr() if n else None
-
-
-def _token_dense(t, what, shape, dtype):
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == tuple(shape)
-            and t.device.index == torch.cuda.current_device()):
-        raise TypeError(f"{what}: expected a contiguous CUDA tensor {list(shape)} of {dtype} on the current device")
-    return t.data_ptr() if t.numel() else None
-
-
 def q8_quantize_tokens(x, out=None, scale=None):
     """x: CUDA fp32, fp16 or bf16 [..., C], rows a fixed stride apart.  Returns (codes int8 [..., C], factors fp32 [...]).
     The codes made here have rows on the 16-byte grid: for C off it they are a slice of a wider tensor."""
-    xp, rows, C_, ldx = _token_rows(x, "x", _FLOAT_TYPES)
-    if out is None:
-        out = torch.empty(x.shape[:-1] + ((C_ + 15) // 16 * 16,), dtype=torch.int8, device=x.device)[..., :C_]
-    if scale is None:
-        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    zp, zrows, zc, ldz = _token_rows(out, "out", (torch.int8,))
-    if (zrows, zc) != (rows, C_):
-        raise TypeError("out: expected the shape of x")
-    _check(lib.q8_quantize_tokens(xp, _FLOAT_TYPES[x.dtype], rows, C_, ldx, zp, ldz, _token_vector(scale, "scale", rows), _stream()))
-    return out, scale
+    rc, made = _native.quantize_tokens(x, out, scale)
+    if rc:
+        _check(rc)
+    return made
 
 
 def q8_dequantize_tokens(z, scale, out_type=Q8_F32, out=None):
-    """z: CUDA int8 [..., C], rows a fixed stride apart; scale: CUDA fp32, one factor per row."""
-    zp, rows, C_, ldz = _token_rows(z, "z", (torch.int8,))
-    if out is None:
-        out = torch.empty(z.shape, dtype=TORCH_DTYPES[out_type], device=z.device)
-    rp, rrows, rc, ldr = _token_rows(out, "out", _FLOAT_TYPES)
-    if (rrows, rc) != (rows, C_):
-        raise TypeError("out: expected the shape of z")
-    _check(lib.q8_dequantize_tokens(zp, rows, C_, ldz, _token_vector(scale, "scale", rows), rp, _FLOAT_TYPES[out.dtype], ldr, _stream()))
-    return out
+    """z: CUDA int8 [..., C], rows a fixed stride apart; scale: CUDA fp32, one factor per row.  Returns scale * z as out_type."""
+    rc, made = _native.dequantize_tokens(z, scale, out_type, out)
+    if rc:
+        _check(rc)
+    return made
 
 
 def q8_linear_workspace_bytes(d):
@@ -551,23 +501,10 @@ def q8_linear(x, w, w_scale, x_scale=None, bias=None, out_type=Q8_BF16, out=None
     """y[..., k] = (sum_c codes * w) * x_scale * w_scale + bias.  x: CUDA int8 codes [..., C] with x_scale, one factor per row, or
     fp32, fp16 or bf16 activations without; w: CUDA int8 [K, C], w_scale and bias: CUDA fp32 [K].  Rows of x, w and out a
     fixed stride apart.  The workspace is made here unless one is given (a uint8 tensor; an empty one: none)."""
-    xp, M, C_, ldx = _token_rows(x, "x", (torch.int8, *_FLOAT_TYPES))
-    wp, K, wc, ldw = _token_rows(w, "w", (torch.int8,))
-    if w.dim() != 2 or wc != C_:
-        raise TypeError("w: expected [K, C]")
-    if out is None:
-        out = torch.empty(x.shape[:-1] + (K,), dtype=TORCH_DTYPES[out_type], device=x.device)
-    yp, yrows, yc, ldy = _token_rows(out, "out", _FLOAT_TYPES)
-    if (yrows, yc) != (M, K):
-        raise TypeError("out: expected [..., K]")
-    d = q8_linear_desc(ldx, ldw, ldy, M, C_, K, Q8_S8 if x.dtype == torch.int8 else _FLOAT_TYPES[x.dtype], _FLOAT_TYPES[out.dtype], 0)
-    if workspace is None:
-        n = q8_linear_workspace_bytes(d)
-        workspace = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
-    wsp, wsn = (None, 0) if workspace is None else (_token_vector(workspace, "workspace", workspace.numel(), torch.uint8), workspace.numel())
-    _check(lib.q8_linear(C.byref(d), xp, _token_vector(x_scale, "x_scale", M), wp, _token_vector(w_scale, "w_scale", K),
-                         _token_vector(bias, "bias", K), yp, wsp, wsn, _stream()))
-    return out
+    rc, made = _native.linear(x, w, w_scale, x_scale, bias, out_type, out, workspace)
+    if rc:
+        _check(rc)
+    return made
 
 
 def q8_moe_workspace_bytes(d):
@@ -580,27 +517,7 @@ def q8_moe(x, router, w_gate_up, s_gate_up, w_down, s_down, top_k, renormalize=T
     """x: CUDA fp32, fp16 or bf16 [..., C], rows a fixed stride apart; router: fp32 [E, C]; w_gate_up: int8 [E, 2 I, C] with s_gate_up
     fp32 [E, 2 I]; w_down: int8 [E, C, I] with s_down fp32 [E, C].  Returns (y [..., C] of x's type, the chosen experts int32
     [..., top_k], best first, and their weights fp32 [..., top_k])."""
-    xp, T, C_, ldx = _token_rows(x, "x", _FLOAT_TYPES)
-    if not (isinstance(w_down, torch.Tensor) and w_down.dim() == 3):
-        raise TypeError("w_down: expected [E, C, I]")
-    E, _, I_ = (int(v) for v in w_down.shape)
-    tensors = (_token_dense(router, "router", (E, C_), torch.float32), _token_dense(w_gate_up, "w_gate_up", (E, 2 * I_, C_), torch.int8),
-               _token_dense(s_gate_up, "s_gate_up", (E, 2 * I_), torch.float32), _token_dense(w_down, "w_down", (E, C_, I_), torch.int8),
-               _token_dense(s_down, "s_down", (E, C_), torch.float32))
-    if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    yp, yrows, yc, ldy = _token_rows(out, "out", (x.dtype,))
-    if (yrows, yc) != (T, C_):
-        raise TypeError("out: expected the shape of x")
-    d = q8_moe_desc(ldx, ldy, T, C_, I_, E, top_k, _FLOAT_TYPES[x.dtype], int(renormalize), 0)
-    nbytes = q8_moe_workspace_bytes(d)
-    if ids is None:
-        ids = torch.empty(x.shape[:-1] + (top_k,), dtype=torch.int32, device=x.device)
-    if probs is None:
-        probs = torch.empty(x.shape[:-1] + (top_k,), dtype=torch.float32, device=x.device)
-    if workspace is None:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
-    _check(lib.q8_moe(C.byref(d), xp, *tensors, yp, _token_vector(ids, "ids", T * top_k, torch.int32),
-                      _token_vector(probs, "probs", T * top_k), _token_vector(workspace, "workspace", workspace.numel(), torch.uint8),
-                      workspace.numel(), _stream()))
-    return out, ids, probs
+    rc, made = _native.moe(x, router, w_gate_up, s_gate_up, w_down, s_down, top_k, renormalize, out, ids, probs, workspace)
+    if rc:
+        _check(rc)
+    return made

@@ -3,10 +3,12 @@
 // binding.py, which holds the declarations and everything that is called rarely; a call through ctypes costs its eleven
 // conversions (q8_conv2d of the smallest layer 7.0 us of host time, detection output with six sources 52 us).
 #include <Python.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
+#include <ATen/ops/empty.h>
 
 #include <cstdint>
 #include <vector>
@@ -24,6 +26,12 @@ struct Entry {
   decltype(&q8_dequantize) dequantize;
   decltype(&q8_detection_output_workspace_bytes) det_bytes;
   decltype(&q8_detection_output) detect;
+  decltype(&q8_quantize_tokens) quantize_tokens;
+  decltype(&q8_dequantize_tokens) dequantize_tokens;
+  decltype(&q8_linear_workspace_bytes) linear_bytes;
+  decltype(&q8_linear) linear;
+  decltype(&q8_moe_workspace_bytes) moe_bytes;
+  decltype(&q8_moe) moe;
 } g_q8;
 
 void* current_stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
@@ -65,6 +73,16 @@ PyObject* call(F f) {
   rc = f();
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
+}
+
+// The same for a call whose status the caller goes on with.
+template <typename F>
+int unlocked(F f) {
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = f();
+  Py_END_ALLOW_THREADS
+  return rc;
 }
 
 bool number(PyObject* o, float* v) {
@@ -294,17 +312,265 @@ PyObject* py_detect(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- token operators: tensors of rows a fixed stride apart, outputs made here where none are given
+
+int float_type(at::ScalarType t) { return t == at::kFloat ? Q8_F32 : (t == at::kHalf ? Q8_F16 : (t == at::kBFloat16 ? Q8_BF16 : -1)); }
+bool scalar_of(int type, at::ScalarType* t) {
+  switch (type) {
+    case Q8_F32: *t = at::kFloat; return true;
+    case Q8_F16: *t = at::kHalf; return true;
+    case Q8_BF16: *t = at::kBFloat16; return true;
+    default: return false;
+  }
+}
+
+enum Kinds { kFloats = 1, kCodes = 2 };
+
+// A CUDA tensor [..., C] on the current device whose rows lie a fixed stride apart (contiguous, or a slice of the last dimension
+// of a wider tensor).  type: Q8_S8 or a floating-point type.
+struct Rows {
+  void* p = nullptr;
+  int64_t rows = 0, C = 0, ld = 0;
+  int type = -1;
+  const at::Tensor* t = nullptr;
+
+  bool parse(PyObject* o, const char* what, int kinds) {
+    t = THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr;
+    if (t && t->is_cuda()) {
+      type = t->scalar_type() == at::kChar ? (int)Q8_S8 : float_type(t->scalar_type());
+      if (!(type == Q8_S8 ? kinds & kCodes : kinds & kFloats)) type = -1;
+    }
+    if (!t || type < 0 || t->dim() < 1) {
+      PyErr_Format(PyExc_TypeError, "%s: expected a CUDA tensor of %s with at least one dimension", what,
+                   kinds == kCodes ? "int8" : (kinds == kFloats ? "fp32, fp16 or bf16" : "int8, fp32, fp16 or bf16"));
+      return false;
+    }
+    if (t->device().index() != c10::cuda::current_device()) { PyErr_Format(PyExc_TypeError, "%s: expected a tensor on the current device", what); return false; }
+    const int64_t d = t->dim();
+    C = ld = t->size(d - 1);
+    if (t->numel() == 0) return true;
+    if (C > 1 && t->stride(d - 1) != 1) { PyErr_Format(PyExc_TypeError, "%s: expected unit stride in the last dimension", what); return false; }
+    rows = 1;
+    for (int64_t i = d - 2; i >= 0; --i) {
+      if (t->size(i) == 1) continue;
+      if (rows == 1) {
+        ld = t->stride(i);
+      } else if (t->stride(i) != ld * rows) {
+        PyErr_Format(PyExc_TypeError, "%s: rows are not a fixed stride apart", what);
+        return false;
+      }
+      rows *= t->size(i);
+    }
+    if (rows > 1 && ld < C) { PyErr_Format(PyExc_TypeError, "%s: rows overlap", what); return false; }
+    p = t->data_ptr();
+    return true;
+  }
+};
+
+// Address of a contiguous CUDA tensor of n values of type `st` on the current device; None: null where that is allowed.
+bool values(PyObject* o, const char* what, int64_t n, at::ScalarType st, const char* st_name, bool optional, void** p) {
+  *p = nullptr;
+  if (optional && o == Py_None) return true;
+  const at::Tensor* t = THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr;
+  if (!t || !t->is_cuda() || t->scalar_type() != st || !t->is_contiguous() || t->numel() != n || t->device().index() != c10::cuda::current_device()) {
+    PyErr_Format(PyExc_TypeError, "%s: expected a contiguous CUDA tensor of %lld %s values on the current device", what, (long long)n, st_name);
+    return false;
+  }
+  *p = n ? t->data_ptr() : nullptr;
+  return true;
+}
+// ... of the shape given.
+bool dense(PyObject* o, const char* what, at::IntArrayRef shape, at::ScalarType st, const char* st_name, void** p) {
+  const at::Tensor* t = THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr;
+  if (!t || t->sizes() != shape) {
+    PyErr_Format(PyExc_TypeError, "%s: expected another shape", what);
+    return false;
+  }
+  return values(o, what, t->numel(), st, st_name, false, p);
+}
+
+// The tensor given, or a new one like those of `like` with sizes[..., last].
+at::Tensor made(const at::Tensor& like, int64_t last, at::ScalarType st) {
+  auto sizes = like.sizes().vec();
+  sizes.back() = last;
+  return at::empty(sizes, like.options().dtype(st).requires_grad(false));
+}
+at::Tensor made_scalar_per_row(const at::Tensor& like, at::ScalarType st) {
+  return at::empty(like.sizes().slice(0, like.dim() - 1), like.options().dtype(st).requires_grad(false));
+}
+
+// The interpreter's status for a call that has written `result` (stolen): (status, result).
+PyObject* answer(int rc, PyObject* result) {
+  if (!result) return nullptr;
+  PyObject* t = Py_BuildValue("(iN)", rc, result);
+  return t;
+}
+
+// (x, out, scale) -> (status, (out, scale))
+PyObject* py_quantize_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!count(n, 3)) return nullptr;
+  HANDLE_TH_ERRORS
+  Rows x, z;
+  if (!x.parse(a[0], "x", kFloats)) return nullptr;
+  THPObjectPtr out, scale;
+  if (a[1] == Py_None) {
+    const at::Tensor wide = made(*x.t, (x.C + 15) / 16 * 16, at::kChar);
+    out = THPVariable_Wrap(x.C % 16 ? wide.narrow(-1, 0, x.C) : wide);
+  } else {
+    out = Py_NewRef(a[1]);
+  }
+  scale = a[2] == Py_None ? THPVariable_Wrap(made_scalar_per_row(*x.t, at::kFloat)) : Py_NewRef(a[2]);
+  if (!out || !scale) return nullptr;
+  void* s;
+  if (!z.parse(out.get(), "out", kCodes)) return nullptr;
+  if (z.rows != x.rows || z.C != x.C) { PyErr_SetString(PyExc_TypeError, "out: expected the shape of x"); return nullptr; }
+  if (!values(scale.get(), "scale", x.rows, at::kFloat, "fp32", false, &s)) return nullptr;
+  void* stream = current_stream();
+  const int rc = unlocked([&] {
+    return g_q8.quantize_tokens(x.p, x.type, (size_t)x.rows, (size_t)x.C, (size_t)x.ld, static_cast<int8_t*>(z.p), (size_t)z.ld, static_cast<float*>(s), stream);
+  });
+  return answer(rc, PyTuple_Pack(2, out.get(), scale.get()));
+  END_HANDLE_TH_ERRORS
+}
+
+// (z, scale, out_type, out) -> (status, out)
+PyObject* py_dequantize_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!count(n, 4)) return nullptr;
+  HANDLE_TH_ERRORS
+  Rows z, r;
+  int type;
+  void* s;
+  if (!z.parse(a[0], "z", kCodes) || !number(a[2], &type) || !values(a[1], "scale", z.rows, at::kFloat, "fp32", false, &s)) return nullptr;
+  THPObjectPtr out;
+  if (a[3] == Py_None) {
+    at::ScalarType st;
+    if (!scalar_of(type, &st)) { PyErr_SetString(PyExc_ValueError, "out_type must be Q8_F32, Q8_F16 or Q8_BF16"); return nullptr; }
+    out = THPVariable_Wrap(made(*z.t, z.C, st));
+  } else {
+    out = Py_NewRef(a[3]);
+  }
+  if (!out || !r.parse(out.get(), "out", kFloats)) return nullptr;
+  if (r.rows != z.rows || r.C != z.C) { PyErr_SetString(PyExc_TypeError, "out: expected the shape of z"); return nullptr; }
+  void* stream = current_stream();
+  const int rc = unlocked([&] {
+    return g_q8.dequantize_tokens(static_cast<const int8_t*>(z.p), (size_t)z.rows, (size_t)z.C, (size_t)z.ld, static_cast<const float*>(s), r.p, r.type,
+                                  (size_t)r.ld, stream);
+  });
+  return answer(rc, out.release());
+  END_HANDLE_TH_ERRORS
+}
+
+bool fits_int(int64_t v, const char* what) {
+  if (v <= 0x7fffffff) return true;
+  PyErr_Format(PyExc_ValueError, "%s: too large", what);
+  return false;
+}
+
+// A workspace of `need` bytes: the tensor given, or one made here (held by *own until the call is enqueued).
+bool workspace_of(PyObject* o, size_t need, const at::Tensor& like, at::Tensor* own, void** p, size_t* bytes) {
+  if (o == Py_None) {
+    *p = nullptr;
+    *bytes = need;
+    if (need) {
+      *own = at::empty({(int64_t)need}, like.options().dtype(at::kByte).requires_grad(false));
+      *p = own->data_ptr();
+    }
+    return true;
+  }
+  if (!THPVariable_Check(o)) { PyErr_SetString(PyExc_TypeError, "workspace: expected a tensor"); return false; }
+  *bytes = (size_t)THPVariable_Unpack(o).numel();
+  return values(o, "workspace", (int64_t)*bytes, at::kByte, "uint8", false, p);
+}
+
+// (x, w, w_scale, x_scale, bias, out_type, out, workspace) -> (status, out)
+PyObject* py_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!count(n, 8)) return nullptr;
+  HANDLE_TH_ERRORS
+  Rows x, w, y;
+  int type;
+  void *ws, *xs, *bias, *space;
+  if (!x.parse(a[0], "x", kFloats | kCodes) || !w.parse(a[1], "w", kCodes) || !number(a[5], &type)) return nullptr;
+  if (w.t->dim() != 2 || w.C != x.C) { PyErr_SetString(PyExc_TypeError, "w: expected [K, C]"); return nullptr; }
+  const int64_t K = w.t->size(0);
+  if (!values(a[2], "w_scale", K, at::kFloat, "fp32", false, &ws) || !values(a[3], "x_scale", x.rows, at::kFloat, "fp32", true, &xs) ||
+      !values(a[4], "bias", K, at::kFloat, "fp32", true, &bias) || !fits_int(x.rows, "x") || !fits_int(K, "w") || !fits_int(x.C, "x"))
+    return nullptr;
+  THPObjectPtr out;
+  if (a[6] == Py_None) {
+    at::ScalarType st;
+    if (!scalar_of(type, &st)) { PyErr_SetString(PyExc_ValueError, "out_type must be Q8_F32, Q8_F16 or Q8_BF16"); return nullptr; }
+    out = THPVariable_Wrap(made(*x.t, K, st));
+  } else {
+    out = Py_NewRef(a[6]);
+  }
+  if (!out || !y.parse(out.get(), "out", kFloats)) return nullptr;
+  if (y.rows != x.rows || y.C != K) { PyErr_SetString(PyExc_TypeError, "out: expected [..., K]"); return nullptr; }
+  const q8_linear_desc d{x.ld, w.ld, y.ld, (int32_t)x.rows, (int32_t)x.C, (int32_t)K, x.type, y.type, 0};
+  size_t need = 0, bytes = 0;
+  at::Tensor own;
+  int rc = a[7] == Py_None ? g_q8.linear_bytes(&d, &need) : Q8_OK;
+  if (rc == Q8_OK) {
+    if (!workspace_of(a[7], need, *x.t, &own, &space, &bytes)) return nullptr;
+    void* stream = current_stream();
+    rc = unlocked([&] {
+      return g_q8.linear(&d, x.p, static_cast<const float*>(xs), static_cast<const int8_t*>(w.p), static_cast<const float*>(ws), static_cast<const float*>(bias),
+                         y.p, space, bytes, stream);
+    });
+  }
+  return answer(rc, out.release());
+  END_HANDLE_TH_ERRORS
+}
+
+// (x, router, w_gate_up, s_gate_up, w_down, s_down, top_k, renormalize, out, ids, probs, workspace) -> (status, (out, ids, probs))
+PyObject* py_moe(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!count(n, 12)) return nullptr;
+  HANDLE_TH_ERRORS
+  Rows x, y;
+  int top_k, renorm = PyObject_IsTrue(a[7]);
+  if (renorm < 0 || !x.parse(a[0], "x", kFloats) || !number(a[6], &top_k)) return nullptr;
+  const at::Tensor* wd = THPVariable_Check(a[4]) ? &THPVariable_Unpack(a[4]) : nullptr;
+  if (!wd || wd->dim() != 3) { PyErr_SetString(PyExc_TypeError, "w_down: expected [E, C, I]"); return nullptr; }
+  const int64_t E = wd->size(0), I = wd->size(2), C = x.C;
+  void *router, *wgu, *sgu, *wdp, *sd, *ids, *probs, *space;
+  if (!dense(a[1], "router", {E, C}, at::kFloat, "fp32", &router) || !dense(a[2], "w_gate_up", {E, 2 * I, C}, at::kChar, "int8", &wgu) ||
+      !dense(a[3], "s_gate_up", {E, 2 * I}, at::kFloat, "fp32", &sgu) || !dense(a[4], "w_down", {E, C, I}, at::kChar, "int8", &wdp) ||
+      !dense(a[5], "s_down", {E, C}, at::kFloat, "fp32", &sd) || !fits_int(x.rows, "x") || !fits_int(E, "router") || !fits_int(C, "x") || !fits_int(I, "w_down"))
+    return nullptr;
+  q8_moe_desc d{x.ld, 0, (int32_t)x.rows, (int32_t)C, (int32_t)I, (int32_t)E, top_k, x.type, renorm, 0};
+  size_t need = 0, bytes = 0;
+  int rc = g_q8.moe_bytes(&d, &need);
+  if (rc != Q8_OK) return answer(rc, Py_NewRef(Py_None));
+  THPObjectPtr out, o_ids, o_probs;
+  out = a[8] == Py_None ? THPVariable_Wrap(made(*x.t, C, x.t->scalar_type())) : Py_NewRef(a[8]);
+  o_ids = a[9] == Py_None ? THPVariable_Wrap(made(*x.t, top_k, at::kInt)) : Py_NewRef(a[9]);
+  o_probs = a[10] == Py_None ? THPVariable_Wrap(made(*x.t, top_k, at::kFloat)) : Py_NewRef(a[10]);
+  if (!out || !o_ids || !o_probs || !y.parse(out.get(), "out", kFloats)) return nullptr;
+  if (y.rows != x.rows || y.C != C || y.type != x.type) { PyErr_SetString(PyExc_TypeError, "out: expected the shape and type of x"); return nullptr; }
+  if (!values(o_ids.get(), "ids", x.rows * top_k, at::kInt, "int32", false, &ids) || !values(o_probs.get(), "probs", x.rows * top_k, at::kFloat, "fp32", false, &probs))
+    return nullptr;
+  d.ldy = y.ld;
+  at::Tensor own;
+  if (!workspace_of(a[11], need, *x.t, &own, &space, &bytes)) return nullptr;
+  void* stream = current_stream();
+  rc = unlocked([&] {
+    return g_q8.moe(&d, x.p, static_cast<const float*>(router), static_cast<const int8_t*>(wgu), static_cast<const float*>(sgu), static_cast<const int8_t*>(wdp),
+                    static_cast<const float*>(sd), y.p, static_cast<int32_t*>(ids), static_cast<float*>(probs), space, bytes, stream);
+  });
+  return answer(rc, PyTuple_Pack(3, out.get(), o_ids.get(), o_probs.get()));
+  END_HANDLE_TH_ERRORS
+}
+
 // (addresses of the entry points, in the order of Entry, the descriptors' class)
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!count(n, 8)) return nullptr;
-  void* p[7];
-  for (int i = 0; i < 7; ++i) {
+  if (!count(n, 14)) return nullptr;
+  void* p[13];
+  for (int i = 0; i < 13; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (!p[i]) return nullptr;
   }
   PyObject* old = g_desc_type;
-  Py_INCREF(a[7]);
-  g_desc_type = a[7];
+  Py_INCREF(a[13]);
+  g_desc_type = a[13];
   Py_XDECREF(old);
   g_q8.conv2d = reinterpret_cast<decltype(g_q8.conv2d)>(p[0]);
   g_q8.then_1x1 = reinterpret_cast<decltype(g_q8.then_1x1)>(p[1]);
@@ -313,6 +579,12 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   g_q8.dequantize = reinterpret_cast<decltype(g_q8.dequantize)>(p[4]);
   g_q8.det_bytes = reinterpret_cast<decltype(g_q8.det_bytes)>(p[5]);
   g_q8.detect = reinterpret_cast<decltype(g_q8.detect)>(p[6]);
+  g_q8.quantize_tokens = reinterpret_cast<decltype(g_q8.quantize_tokens)>(p[7]);
+  g_q8.dequantize_tokens = reinterpret_cast<decltype(g_q8.dequantize_tokens)>(p[8]);
+  g_q8.linear_bytes = reinterpret_cast<decltype(g_q8.linear_bytes)>(p[9]);
+  g_q8.linear = reinterpret_cast<decltype(g_q8.linear)>(p[10]);
+  g_q8.moe_bytes = reinterpret_cast<decltype(g_q8.moe_bytes)>(p[11]);
+  g_q8.moe = reinterpret_cast<decltype(g_q8.moe)>(p[12]);
   Py_RETURN_NONE;
 }
 
@@ -320,6 +592,8 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {Q8_METHOD("bind", py_bind),         Q8_METHOD("conv2d", py_conv2d),     Q8_METHOD("then_1x1", py_then_1x1),
                          Q8_METHOD("maxabs", py_maxabs),     Q8_METHOD("quantize", py_quantize), Q8_METHOD("dequantize", py_dequantize),
                          Q8_METHOD("detect", py_detect),     Q8_METHOD("detect_size", py_detect_size),
+                         Q8_METHOD("quantize_tokens", py_quantize_tokens), Q8_METHOD("dequantize_tokens", py_dequantize_tokens),
+                         Q8_METHOD("linear", py_linear),     Q8_METHOD("moe", py_moe),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_q8native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
