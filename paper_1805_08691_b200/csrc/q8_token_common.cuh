@@ -53,6 +53,95 @@ __device__ __forceinline__ int token_code(float x, const TokenFactor& f) {
   return min(max(__float2int_rn(y), -128), 127);
 }
 
+// Packed fp32 arithmetic: two independent IEEE operations an instruction.
+__device__ __forceinline__ unsigned long long two(float a, float b) {
+  unsigned long long d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ void both(unsigned long long d, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(d)); }
+__device__ __forceinline__ unsigned long long mul_two(unsigned long long a, unsigned long long b) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ unsigned long long add_two(unsigned long long a, unsigned long long b) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ unsigned long long fma_two(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+
+// Four codes of a finite token, the first in the lowest byte; the same as token_code.  The conversion to an integer is a sum
+// with 1.5 * 2^23, whose low bits then hold the rounded quotient (a conversion instruction runs at an eighth of the rate).
+// f.general is the same for all lanes.
+__device__ __forceinline__ unsigned codes_4(const float (&x)[4], const TokenFactor& f) {
+  if (f.general) {
+    unsigned w = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w |= ((unsigned)token_code(x[j], f) & 255u) << (8 * j);
+    return w;
+  }
+  const unsigned long long r = two(f.r, f.r), s = two(-f.s, -f.s), magic = two(12582912.0f, 12582912.0f);
+  unsigned t[4];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const unsigned long long v = two(x[2 * j], x[2 * j + 1]);
+    unsigned long long y = mul_two(v, r);
+    y = fma_two(fma_two(y, s, v), r, y);
+    y = fma_two(fma_two(y, s, v), r, y);
+    float a, b;
+    both(add_two(y, magic), a, b);
+    t[2 * j] = __float_as_uint(a);
+    t[2 * j + 1] = __float_as_uint(b);
+  }
+  return __byte_perm(__byte_perm(t[0], t[1], 0x0040), __byte_perm(t[2], t[3], 0x0040), 0x5410);
+}
+
+// Four codes of a word as floats times s.
+__device__ __forceinline__ void values_4(unsigned w, float s, float (&v)[4]) {
+  // byte b -> 2^23 + 128 + code without a conversion instruction
+  const unsigned u = w ^ 0x80808080u;
+  const unsigned long long magic = two(-8388736.0f, -8388736.0f), s2 = two(s, s);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float a = __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7540u | (unsigned)(2 * j)));
+    const float b = __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7540u | (unsigned)(2 * j + 1)));
+    both(mul_two(add_two(two(a, b), magic), s2), v[2 * j], v[2 * j + 1]);
+  }
+}
+
+// Pairs of 16-bit floats as fp32 and back, and the larger of their magnitudes by halves (bits of magnitudes order like
+// integers, NaN above infinity).
+template <typename T> __device__ __forceinline__ void unpack_two(unsigned w, float& a, float& b);
+template <> __device__ __forceinline__ void unpack_two<__nv_bfloat16>(unsigned w, float& a, float& b) {
+  a = __uint_as_float(w << 16);
+  b = __uint_as_float(w & 0xffff0000u);
+}
+template <> __device__ __forceinline__ void unpack_two<__half>(unsigned w, float& a, float& b) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+  a = f.x;
+  b = f.y;
+}
+template <typename T> __device__ __forceinline__ unsigned pack_two(float a, float b);
+template <> __device__ __forceinline__ unsigned pack_two<__nv_bfloat16>(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const unsigned*>(&h);
+}
+template <> __device__ __forceinline__ unsigned pack_two<__half>(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const unsigned*>(&h);
+}
+__device__ __forceinline__ unsigned max_two(unsigned m, unsigned w) {
+  unsigned d;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(m), "r"(w & 0x7fff7fffu));
+  return d;
+}
+
 // Bytes pos .. pos + 15 of a row of `len` bytes, zero from len on; no byte outside the row is read.  kAligned: the row
 // starts on the 16-byte grid and so does pos.
 template <bool kAligned>

@@ -1,41 +1,228 @@
 // Codes and factors of tokens (q8_quantize_tokens) and the way back (q8_dequantize_tokens).
 //
-// A block takes one token: it holds the row's values in registers between the maximum and the codes, so that they are
-// read from memory once; values beyond kHeld per thread are read a second time, from L2.  Bound by memory.
+// Bound by memory.  A team of threads (a warp, or a block of 128 or 512) takes a token and holds its values in registers between
+// the maximum and the codes, so that they are read from memory once; what a team cannot hold is read a second time, from L2.
+// A thread takes 16 bytes of a row at a time where rows lie on the 16-byte grid, else four values.  Teams are as large as
+// leaves a thread about four of these (64 bytes in flight each, 128 KiB an SM), and with fewer tokens than that occupies the
+// GPU large enough for one each: one token of 4096 values is then a few microseconds of latency and nothing else.
+// 8192 x 4096 bf16: 47 -> FIGQ us to codes (FIGQB TB/s), FIGD us back (FIGDB TB/s); the first form here, a block a token that
+// read its row twice, value by value, 73 us for both.
 #include "q8_token_common.cuh"
 
 namespace q8 {
 namespace {
 
-constexpr int kTokThreads = 256;
+constexpr int kHeld = 4;  // chunks a thread holds
 
-template <typename T>
-__global__ void __launch_bounds__(kTokThreads) quantize_tokens_kernel(const T* __restrict__ x, size_t tokens, size_t C, size_t ldx,
-                                                                      signed char* __restrict__ z, size_t ldz, float* __restrict__ scale) {
-  __shared__ unsigned int part[kTokThreads / 32];
-  for (size_t t = blockIdx.x; t < tokens; t += gridDim.x) {
-    const T* row = x + t * ldx;
-    unsigned int m = 0;
-    for (size_t c = threadIdx.x; c < C; c += kTokThreads) m = max(m, abs_word(to_f32(row[c])));
-    m = warp_max(m);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
-    __syncthreads();
+// Sixteen bytes of a row (V values), or four values where rows do not lie on that grid; those from C on are zero.
+template <typename T, bool kVec>
+struct Chunk {
+  static constexpr int V = kVec ? 16 / (int)sizeof(T) : 4;
+  unsigned w[V * sizeof(T) / 4];
+  __device__ __forceinline__ void load(const T* row, size_t c, size_t C) {
+    if (kVec && c + V <= C) {
+      *reinterpret_cast<uint4*>(w) = __ldg(reinterpret_cast<const uint4*>(row + c));
+    } else {
 #pragma unroll
-    for (int i = 0; i < kTokThreads / 32; ++i) m = max(m, part[i]);
-    const TokenFactor f = token_factor(m);
-    if (threadIdx.x == 0) scale[t] = f.s;
-    for (size_t c = threadIdx.x; c < C; c += kTokThreads) z[t * ldz + c] = (signed char)token_code(to_f32(row[c]), f);
+      for (int j = 0; j < V; ++j) {
+        const bool live = c + j < C;
+        if constexpr (sizeof(T) == 4) {
+          w[j] = live ? reinterpret_cast<const unsigned*>(row)[c + j] : 0u;
+        } else {
+          const unsigned h = live ? reinterpret_cast<const unsigned short*>(row)[c + j] : 0u;
+          w[j / 2] = j & 1 ? w[j / 2] | h << 16 : h;
+        }
+      }
+    }
+  }
+  // running maximum of magnitudes: of words, or of the halves of words
+  __device__ __forceinline__ void max_into(unsigned& m) const {
+#pragma unroll
+    for (int j = 0; j < (int)(V * sizeof(T) / 4); ++j) {
+      if constexpr (sizeof(T) == 4) m = max(m, w[j] & 0x7fffffffu);
+      else m = max_two(m, w[j]);
+    }
+  }
+  // z: the row's codes; aligned: V codes can be written at once
+  __device__ __forceinline__ void store(signed char* z, size_t c, size_t C, const TokenFactor& f, bool aligned) const {
+    unsigned o[V / 4];
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) {
+      float v[4];
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = __uint_as_float(w[4 * j + q]);
+      } else {
+        unpack_two<T>(w[2 * j], v[0], v[1]);
+        unpack_two<T>(w[2 * j + 1], v[2], v[3]);
+      }
+      o[j] = f.finite ? codes_4(v, f) : 0u;
+    }
+    if (aligned && c + V <= C) {
+      if constexpr (V == 8) *reinterpret_cast<uint2*>(z + c) = make_uint2(o[0], o[1]);
+      else *reinterpret_cast<unsigned*>(z + c) = o[0];
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (c + j < C) z[c + j] = (signed char)(o[j / 4] >> (8 * (j & 3)));
+    }
+  }
+};
+template <typename T>
+__device__ __forceinline__ unsigned as_fp32_bits(unsigned m) {  // of a maximum of halves
+  if constexpr (sizeof(T) == 4) {
+    return m;
+  } else {
+    float a, b;
+    unpack_two<T>(max(m & 0xffffu, m >> 16), a, b);
+    return __float_as_uint(a);
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kTokThreads) dequantize_tokens_kernel(const signed char* __restrict__ z, size_t tokens, size_t C, size_t ldz,
-                                                                        const float* __restrict__ scale, T* __restrict__ r, size_t ldr) {
-  for (size_t t = blockIdx.x; t < tokens; t += gridDim.x) {
-    const float s = scale[t];
-    for (size_t c = threadIdx.x; c < C; c += kTokThreads) r[t * ldr + c] = from_f32<T>(__fmul_rn(s, (float)z[t * ldz + c]));
+// Teams of kTeam threads, a token each.  kTeam 32: eight tokens a block.
+template <typename T, bool kVec, int kTeam>
+__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam) quantize_tokens_kernel(const T* __restrict__ x, size_t tokens, size_t C, size_t ldx,
+                                                                                    signed char* __restrict__ z, size_t ldz, float* __restrict__ scale, int z_aligned) {
+  constexpr int V = Chunk<T, kVec>::V;
+  __shared__ unsigned part[kTeam / 32];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int tid = kTeam == 32 ? threadIdx.x & 31 : threadIdx.x;
+  const size_t t = kTeam == 32 ? (size_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x;
+  if (kTeam == 32 && t >= tokens) return;
+  const T* row = x + t * ldx;
+  signed char* out = z + t * ldz;
+  Chunk<T, kVec> held[kHeld];
+  unsigned m = 0;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const size_t c = (size_t)(tid + j * kTeam) * V;
+    if (c < C) held[j].load(row, c, C);
   }
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if ((size_t)(tid + j * kTeam) * V < C) held[j].max_into(m);
+  for (size_t c = (size_t)(tid + kHeld * kTeam) * V; c < C; c += (size_t)kTeam * V) {
+    Chunk<T, kVec> again;
+    again.load(row, c, C);
+    again.max_into(m);
+  }
+  m = warp_max(as_fp32_bits<T>(m));
+  if (kTeam > 32) {
+    if ((tid & 31) == 0) part[tid >> 5] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTeam / 32; ++i) m = max(m, part[i]);
+  }
+  const TokenFactor f = token_factor(m);
+  if (tid == 0) scale[t] = f.s;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const size_t c = (size_t)(tid + j * kTeam) * V;
+    if (c < C) held[j].store(out, c, C, f, z_aligned);
+  }
+  for (size_t c = (size_t)(tid + kHeld * kTeam) * V; c < C; c += (size_t)kTeam * V) {
+    Chunk<T, kVec> again;
+    again.load(row, c, C);
+    again.store(out, c, C, f, z_aligned);
+  }
+}
+
+// Sixteen codes a thread and turn where rows lie on the 16-byte grid, else four.
+template <typename T, bool kVec, int kTeam>
+__global__ void __launch_bounds__(256) dequantize_tokens_kernel(const signed char* __restrict__ z, size_t tokens, size_t C, size_t ldz,
+                                                                const float* __restrict__ scale, T* __restrict__ r, size_t ldr) {
+  constexpr int V = kVec ? 16 : 4;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const size_t t = (size_t)blockIdx.x * (256 / kTeam) + threadIdx.x / kTeam;
+  if (t >= tokens) return;
+  const float s = scale[t];
+  const signed char* in = z + t * ldz;
+  T* out = r + t * ldr;
+  for (size_t c = (size_t)(threadIdx.x % kTeam) * V; c < C; c += (size_t)kTeam * V) {
+    if (kVec && c + V <= C) {
+      const uint4 w = __ldg(reinterpret_cast<const uint4*>(in + c));
+      const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int j = 0; j < 4; j += sizeof(T) == 4 ? 1 : 2) {
+        float v[4], x[4];
+        values_4(u[j], s, v);
+        if constexpr (sizeof(T) == 4) {
+          reinterpret_cast<float4*>(out + c)[j] = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+          values_4(u[j + 1], s, x);
+          reinterpret_cast<uint4*>(out + c)[j / 2] = make_uint4(pack_two<T>(v[0], v[1]), pack_two<T>(v[2], v[3]), pack_two<T>(x[0], x[1]), pack_two<T>(x[2], x[3]));
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (c + j < C) out[c + j] = from_f32<T>(__fmul_rn(s, (float)in[c + j]));
+    }
+  }
+}
+
+template <typename... Params, typename... Args>
+int launch_dependent(const char* name, void (*kernel)(Params...), size_t grid, int threads, cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return check_cuda(cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...), name);
+}
+
+constexpr size_t kMostTokens = 0x7fffffff;  // of a launch
+
+template <typename T, bool kVec>
+int quantize_as(const T* x, size_t tokens, size_t C, size_t ldx, signed char* z, size_t ldz, float* scale, cudaStream_t s) {
+  constexpr int V = Chunk<T, kVec>::V;
+  const int z_aligned = aligned_to(z, V) && ldz % V == 0;
+  const size_t chunks = (C + V - 1) / V;
+  // chunks a thread: about four, one where that leaves fewer than two blocks an SM
+  const size_t want = tokens < (size_t)2 * sm_count() ? chunks : (chunks + 3) / 4;
+  for (size_t t0 = 0; t0 < tokens; t0 += kMostTokens) {
+    const size_t n = tokens - t0 < kMostTokens ? tokens - t0 : kMostTokens;
+    const T* xt = x + t0 * ldx;
+    signed char* zt = z + t0 * ldz;
+    int rc;
+    if (want <= 32) rc = launch_dependent("quantize_tokens_kernel", quantize_tokens_kernel<T, kVec, 32>, (n + 7) / 8, 256, s, xt, n, C, ldx, zt, ldz, scale + t0, z_aligned);
+    else if (want <= 192) rc = launch_dependent("quantize_tokens_kernel", quantize_tokens_kernel<T, kVec, 128>, n, 128, s, xt, n, C, ldx, zt, ldz, scale + t0, z_aligned);
+    else rc = launch_dependent("quantize_tokens_kernel", quantize_tokens_kernel<T, kVec, 512>, n, 512, s, xt, n, C, ldx, zt, ldz, scale + t0, z_aligned);
+    if (rc != Q8_OK) return rc;
+  }
+  return Q8_OK;
+}
+template <typename T>
+int quantize_any(const void* x, size_t tokens, size_t C, size_t ldx, signed char* z, size_t ldz, float* scale, cudaStream_t s) {
+  const T* p = static_cast<const T*>(x);
+  if (aligned16(x) && ldx * sizeof(T) % 16 == 0) return quantize_as<T, true>(p, tokens, C, ldx, z, ldz, scale, s);
+  return quantize_as<T, false>(p, tokens, C, ldx, z, ldz, scale, s);
+}
+
+template <typename T, bool kVec>
+int dequantize_as(const signed char* z, size_t tokens, size_t C, size_t ldz, const float* scale, T* r, size_t ldr, cudaStream_t s) {
+  const size_t chunks = (C + (kVec ? 15 : 3)) / (kVec ? 16 : 4);
+  for (size_t t0 = 0; t0 < tokens; t0 += kMostTokens) {
+    const size_t n = tokens - t0 < kMostTokens ? tokens - t0 : kMostTokens;
+    const signed char* zt = z + t0 * ldz;
+    T* rt = r + t0 * ldr;
+    const int rc = chunks <= 96 ? launch_dependent("dequantize_tokens_kernel", dequantize_tokens_kernel<T, kVec, 32>, (n + 7) / 8, 256, s, zt, n, C, ldz, scale + t0, rt, ldr)
+                                : launch_dependent("dequantize_tokens_kernel", dequantize_tokens_kernel<T, kVec, 256>, n, 256, s, zt, n, C, ldz, scale + t0, rt, ldr);
+    if (rc != Q8_OK) return rc;
+  }
+  return Q8_OK;
+}
+template <typename T>
+int dequantize_any(const signed char* z, size_t tokens, size_t C, size_t ldz, const float* scale, void* r, size_t ldr, cudaStream_t s) {
+  T* p = static_cast<T*>(r);
+  if (aligned16(z) && ldz % 16 == 0 && aligned16(r) && ldr * sizeof(T) % 16 == 0) return dequantize_as<T, true>(z, tokens, C, ldz, scale, p, ldr, s);
+  return dequantize_as<T, false>(z, tokens, C, ldz, scale, p, ldr, s);
 }
 
 int check_tokens(const char* fn, const void* x, int type, size_t tokens, size_t C, size_t ldx, const void* z, size_t ldz, const float* scale) {
@@ -47,16 +234,12 @@ int check_tokens(const char* fn, const void* x, int type, size_t tokens, size_t 
   return Q8_OK;
 }
 
-int token_grid(size_t tokens) { return (int)(tokens < (size_t)sm_count() * 8 ? tokens : (size_t)sm_count() * 8); }
-
 }  // namespace
 
 int launch_quantize_tokens(const void* x, int x_type, size_t tokens, size_t C, size_t ldx, int8_t* z, size_t ldz, float* scale, cudaStream_t s) {
-  const int grid = token_grid(tokens);
-  if (x_type == Q8_F32) quantize_tokens_kernel<float><<<grid, kTokThreads, 0, s>>>(static_cast<const float*>(x), tokens, C, ldx, z, ldz, scale);
-  else if (x_type == Q8_F16) quantize_tokens_kernel<__half><<<grid, kTokThreads, 0, s>>>(static_cast<const __half*>(x), tokens, C, ldx, z, ldz, scale);
-  else quantize_tokens_kernel<__nv_bfloat16><<<grid, kTokThreads, 0, s>>>(static_cast<const __nv_bfloat16*>(x), tokens, C, ldx, z, ldz, scale);
-  return check_launch("quantize_tokens_kernel");
+  if (x_type == Q8_F32) return quantize_any<float>(x, tokens, C, ldx, z, ldz, scale, s);
+  if (x_type == Q8_F16) return quantize_any<__half>(x, tokens, C, ldx, z, ldz, scale, s);
+  return quantize_any<__nv_bfloat16>(x, tokens, C, ldx, z, ldz, scale, s);
 }
 
 }  // namespace q8
@@ -76,12 +259,10 @@ int q8_dequantize_tokens(const int8_t* z, size_t tokens, size_t C, size_t ldz, c
   clear_error();
   const int rc = check_tokens("q8_dequantize_tokens", r, r_type, tokens, C, ldr, z, ldz, d_scale);
   if (rc != Q8_OK || tokens == 0) return rc;
-  const int grid = token_grid(tokens);
   cudaStream_t s = as_stream(stream);
-  if (r_type == Q8_F32) dequantize_tokens_kernel<float><<<grid, kTokThreads, 0, s>>>(z, tokens, C, ldz, d_scale, static_cast<float*>(r), ldr);
-  else if (r_type == Q8_F16) dequantize_tokens_kernel<__half><<<grid, kTokThreads, 0, s>>>(z, tokens, C, ldz, d_scale, static_cast<__half*>(r), ldr);
-  else dequantize_tokens_kernel<__nv_bfloat16><<<grid, kTokThreads, 0, s>>>(z, tokens, C, ldz, d_scale, static_cast<__nv_bfloat16*>(r), ldr);
-  return check_launch("dequantize_tokens_kernel");
+  if (r_type == Q8_F32) return dequantize_any<float>(z, tokens, C, ldz, d_scale, r, ldr, s);
+  if (r_type == Q8_F16) return dequantize_any<__half>(z, tokens, C, ldz, d_scale, r, ldr, s);
+  return dequantize_any<__nv_bfloat16>(z, tokens, C, ldz, d_scale, r, ldr, s);
 }
 
 }  // extern "C"
