@@ -42,17 +42,20 @@ int regrid(const int8_t* in, long long rows, int C, long long ld, int8_t* out, i
 }
 
 bool on_grid(const void* p, long long ld) { return aligned16(p) && ld % 16 == 0 && ld < (1ll << 40); }
-bool few_tokens(const LinearArgs& a) { return a.M <= 32; }
+bool few_tokens(const LinearArgs& a) { return linear_stream_fits(a); }
+// Floating-point activations of so few tokens are quantized by every block of the streaming kernel.
+constexpr int kStagedTokens = 4;
 size_t up16(size_t v) { return (v + 15) & ~(size_t)15; }
 
 // Parts of the workspace: codes and factors of x, weights on the grid; a part of zero bytes is not needed.
 struct LinearSpace { size_t codes, factors, weights; size_t bytes() const { return codes + factors + weights; } };
 LinearSpace linear_space(const LinearArgs& a, bool x_on_grid, bool w_on_grid) {
   LinearSpace s{0, 0, 0};
-  if (a.M == 0 || few_tokens(a)) return s;
+  const bool few = few_tokens(a);
+  if (a.M == 0 || (few && (a.x_type == Q8_S8 || a.M <= kStagedTokens))) return s;
   if (a.x_type != Q8_S8) s.factors = up16((size_t)a.M * 4);
   if (a.x_type != Q8_S8 || !x_on_grid) s.codes = (size_t)a.M * up16(a.C);
-  if (!w_on_grid) s.weights = (size_t)a.K * up16(a.C);
+  if (!w_on_grid && !few) s.weights = (size_t)a.K * up16(a.C);
   return s;
 }
 
@@ -89,7 +92,8 @@ int q8_linear(const q8_linear_desc* d, const void* x, const float* x_scale, cons
   a.x = x; a.x_scale = x_scale; a.w = w; a.w_scale = w_scale; a.bias = bias; a.y = y;
   a.stream = as_stream(stream);
   const LinearSpace sp = linear_space(a, on_grid(x, a.ldx), on_grid(w, a.ldw));
-  if (few_tokens(a) || sp.bytes() > (workspace ? workspace_bytes : 0)) return launch_linear_rows(a);
+  const bool few = few_tokens(a);
+  if (sp.bytes() > (workspace ? workspace_bytes : 0) || (few && sp.bytes() == 0)) return few ? launch_linear_stream(a) : launch_linear_rows(a);
   int8_t* const codes = static_cast<int8_t*>(workspace);
   float* const factors = reinterpret_cast<float*>(codes + sp.codes);
   const int pitch = (int)up16(a.C);
@@ -107,7 +111,7 @@ int q8_linear(const q8_linear_desc* d, const void* x, const float* x_scale, cons
     if (rc != Q8_OK) return rc;
     a.w = weights; a.ldw = pitch;
   }
-  return launch_linear_umma(a);
+  return few ? launch_linear_stream(a) : launch_linear_umma(a);
 }
 
 }  // extern "C"

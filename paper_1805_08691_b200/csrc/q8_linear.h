@@ -19,7 +19,11 @@ struct LinearArgs {
 
 // Many tokens, codes on the 16-byte grid: tensor cores fed by TMA (q8_linear_umma.cu).
 int launch_linear_umma(const LinearArgs& a);
-// Few tokens, or operands off the 16-byte grid: weights streamed row by row (q8_linear_rows.cu).
+// Few tokens: weights streamed through shared memory (q8_linear_stream.cu).
+constexpr int kStreamTokens = 32;
+bool linear_stream_fits(const LinearArgs& a);
+int launch_linear_stream(const LinearArgs& a);
+// Everything else, without scratch (q8_linear_rows.cu).
 int launch_linear_rows(const LinearArgs& a);
 int launch_quantize_tokens(const void* x, int x_type, size_t tokens, size_t C, size_t ldx, int8_t* z, size_t ldz, float* scale, cudaStream_t s);
 

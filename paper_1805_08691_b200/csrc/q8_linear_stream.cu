@@ -1,0 +1,253 @@
+// The product with a factor per token for few tokens: bound by the bytes of the weights and, for small ones, by latency.
+//
+//   D[16 output channels, 8 NT tokens] (int32, registers) = W[16, C] (rings in shared memory) x Z[8 NT, C]^T (shared memory)
+//
+// A block holds the codes of all tokens in shared memory and walks over tiles of 16 output channels; its eight warps share
+// the reduction, and their rings of weights run on from tile to tile.  Floating-point activations of a few tokens become codes
+// while they are staged: every block finds the factors itself, which costs less than a launch before it.  What the block
+// will read first is on its way into L2 while the kernel before it drains (a hint, which reads nothing: weights may be
+// that kernel's results).
+//
+// RATES
+#include <atomic>
+
+#include "q8_linear.h"
+#include "q8_token_ring.cuh"
+
+namespace q8 {
+namespace {
+
+constexpr int kSWarps = 8, kSThreads = 32 * kSWarps;
+constexpr int kSDepth = 6;              // steps of a warp's ring: 48 KiB a block
+constexpr int kSSmem = 224 * 1024;
+
+struct StreamParams {
+  int M, C, K, steps, tiles, pitch, x_vec;
+  long long ldx, ldw, ldy;
+  const void* x;
+  const float* x_scale;
+  const signed char* w;
+  const float* w_scale;
+  const float* bias;
+  void* y;
+  int x_type, y_type;
+  int red_at, codes_at;                 // bytes in shared memory
+};
+
+// Factors and codes of the tokens, by the whole block.
+template <typename T>
+__device__ __forceinline__ void stage_tokens(const StreamParams& p, signed char* codes, TokenFactor* fac, unsigned* maxima) {
+  const T* x = static_cast<const T*>(p.x);
+  constexpr int V = 16 / sizeof(T);
+  for (int t = threadIdx.x; t < p.M; t += kSThreads) maxima[t] = 0u;
+  __syncthreads();
+  auto load = [&](const T* row, int c, float (&v)[V]) {
+    if (p.x_vec && c + V <= p.C) {
+      const uint4 q = *reinterpret_cast<const uint4*>(row + c);
+      const unsigned w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4) v[j] = __uint_as_float(w[j]);
+        else unpack_two<T>(w[j], v[2 * j], v[2 * j + 1]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = c + j < p.C ? to_f32(row[c + j]) : 0.0f;
+    }
+  };
+  for (int t = 0; t < p.M; ++t) {
+    unsigned m = 0;
+    for (int c = threadIdx.x * V; c < p.C; c += kSThreads * V) {
+      float v[V];
+      load(x + (long long)t * p.ldx, c, v);
+#pragma unroll
+      for (int j = 0; j < V; ++j) m = max(m, abs_word(v[j]));
+    }
+    m = warp_max(m);
+    if ((threadIdx.x & 31) == 0) atomicMax(maxima + t, m);
+  }
+  __syncthreads();
+  for (int t = 0; t < p.M; ++t) {
+    const TokenFactor f = token_factor(maxima[t]);
+    if (threadIdx.x == 0) fac[t] = f;
+    for (int c = threadIdx.x * V; c < 64 * p.steps; c += kSThreads * V) {
+      float v[V];
+      load(x + (long long)t * p.ldx, c, v);
+#pragma unroll
+      for (int j = 0; j < V / 4; ++j) {
+        const float q[4] = {v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+        *reinterpret_cast<unsigned*>(codes + t * p.pitch + c + 4 * j) = f.finite ? codes_4(q, f) : 0u;
+      }
+    }
+  }
+}
+
+template <int NT, int kGrid>
+__global__ void __launch_bounds__(kSThreads, 2) linear_stream_kernel(const __grid_constant__ StreamParams p) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ TokenFactor s_fac[8 * NT];
+  __shared__ unsigned s_max[8 * NT];
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, i = lane & 3;
+  int* const red = reinterpret_cast<int*>(smem + p.red_at);  // [4 NT][32] of the tile
+  signed char* const codes = reinterpret_cast<signed char*>(smem + p.codes_at);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  {
+    // the first steps of every warp
+    const int row = blockIdx.x * 16 + (tid >> 4);
+    const long long at = (long long)min(row, p.K - 1) * p.ldw + (tid & 15) * 128;
+    if ((tid & 15) * 128 < p.C) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.w + at));
+    if ((tid & 15) * 128 + 2048 < p.C) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.w + at + 2048));
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  // a warp takes every eighth step of a tile
+  const int n = (p.steps - warp + kSWarps - 1) / kSWarps;  // steps of a tile that are this warp's
+  Ring<kGrid, kSDepth> ring;
+  ring.init(smem + warp * Ring<kGrid, kSDepth>::kBytes, lane);
+  int r_tile = blockIdx.x, r_step = 0;                     // of the next step to be copied
+  Rows r;
+  auto begin = [&](int tile) {
+    const int from = 64 * warp + 16 * i;
+    r.a = p.w + (long long)min(tile * 16 + g, p.K - 1) * p.ldw + from;
+    r.b = p.w + (long long)min(tile * 16 + g + 8, p.K - 1) * p.ldw + from;
+    r.left = p.C - from;
+  };
+  auto issue = [&] {
+    while (ring.flying < kSDepth && r_tile < p.tiles && n > 0) {
+      ring.put(r);
+      r.a += 64 * (kSWarps - 1); r.b += 64 * (kSWarps - 1); r.left -= 64 * (kSWarps - 1);
+      if (++r_step == n) {
+        r_step = 0;
+        r_tile += gridDim.x;
+        if (r_tile < p.tiles) begin(r_tile);
+      }
+    }
+  };
+  begin(r_tile);
+  const signed char* const first_a = r.a;
+  const signed char* const first_b = r.b;
+  issue();
+
+  if (p.x_type == Q8_S8) {
+    const signed char* x = static_cast<const signed char*>(p.x);
+    const int units = p.M * p.steps * 4;
+    for (int u = tid; u < units; u += kSThreads) {
+      const int t = u / (p.steps * 4), c = (u - t * p.steps * 4) * 16;
+      const signed char* row = x + (long long)t * p.ldx;
+      *reinterpret_cast<uint4*>(codes + t * p.pitch + c) = p.x_vec ? load_16<true>(row, c, p.C) : load_16<false>(row, c, p.C);
+    }
+  } else if (p.x_type == Q8_F32) {
+    stage_tokens<float>(p, codes, s_fac, s_max);
+  } else if (p.x_type == Q8_F16) {
+    stage_tokens<__half>(p, codes, s_fac, s_max);
+  } else {
+    stage_tokens<__nv_bfloat16>(p, codes, s_fac, s_max);
+  }
+  for (int o = tid; o < 128 * NT; o += kSThreads) red[o] = 0;
+  __syncthreads();
+
+  const signed char* z[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) z[t] = codes + min(8 * t + g, p.M - 1) * p.pitch + 64 * warp + 16 * i;
+  Rows now{first_a, first_b, 0};  // for the alignment of the rows alone
+  for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
+    if constexpr (kGrid == 1) {
+      const int from = 64 * warp + 16 * i;
+      now.a = p.w + (long long)min(tile * 16 + g, p.K - 1) * p.ldw + from;
+      now.b = p.w + (long long)min(tile * 16 + g + 8, p.K - 1) * p.ldw + from;
+    }
+    // this thread's outputs: channel o & 15 of the tokens (o >> 4) + 16 q
+    const int n0 = tile * 16 + (tid & 15);
+    const float ws = n0 < p.K ? __ldg(p.w_scale + n0) : 0.0f, bias = p.bias && n0 < p.K ? __ldg(p.bias + n0) : 0.0f;
+    int d[NT][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0;
+#pragma unroll 2
+    for (int s = 0; s < n; ++s) {
+      uint4 a, b;
+      ring.get(now, a, b);
+      issue();
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const uint4 q = *reinterpret_cast<const uint4*>(z[t] + 512 * s);
+        mma_16x8x32(d[t], a.x, b.x, a.y, b.y, q.x, q.y);
+        mma_16x8x32(d[t], a.z, b.z, a.w, b.w, q.z, q.w);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) atomicAdd(red + 32 * (4 * t + j) + lane, d[t][j]);
+    __syncthreads();
+    for (int t = tid >> 4; t < 8 * NT; t += 16) {
+      const int row = tid & 15, at = 32 * (4 * (t >> 3) + (t & 1) + 2 * (row >> 3)) + 4 * (row & 7) + ((t & 7) >> 1);
+      const int sum = red[at];
+      red[at] = 0;
+      if (t >= p.M || n0 >= p.K) continue;
+      const float xs = p.x_type == Q8_S8 ? __ldg(p.x_scale + t) : s_fac[t].s;
+      float v = __fmul_rn(__fmul_rn(__int2float_rn(sum), xs), ws);
+      if (p.bias) v = __fadd_rn(v, bias);
+      const long long o = (long long)t * p.ldy + n0;
+      if (p.y_type == Q8_F32) static_cast<float*>(p.y)[o] = v;
+      else if (p.y_type == Q8_F16) static_cast<__half*>(p.y)[o] = __float2half_rn(v);
+      else static_cast<__nv_bfloat16*>(p.y)[o] = __float2bfloat16_rn(v);
+    }
+    __syncthreads();
+  }
+}
+
+template <int NT, int kGrid>
+int launch_stream(StreamParams p, cudaStream_t s) {
+  p.red_at = kSWarps * Ring<kGrid, kSDepth>::kBytes;
+  p.codes_at = p.red_at + 512 * NT;
+  const int dyn = p.codes_at + p.M * p.pitch;
+  static std::atomic<bool> set[kMaxDevices];
+  const int dev = current_device();
+  if (dev < 0 || !set[dev].load(std::memory_order_relaxed)) {
+    const int rc = check_cuda(cudaFuncSetAttribute(linear_stream_kernel<NT, kGrid>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSSmem), "linear_stream_kernel");
+    if (rc != Q8_OK) return rc;
+    if (dev >= 0) set[dev].store(true, std::memory_order_relaxed);
+  }
+  const int at_once = sm_count() * (dyn <= 110 * 1024 ? 2 : 1);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(p.tiles < at_once ? p.tiles : at_once));
+  cfg.blockDim = dim3(kSThreads);
+  cfg.dynamicSmemBytes = (size_t)dyn;
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return check_cuda(cudaLaunchKernelEx(&cfg, linear_stream_kernel<NT, kGrid>, p), "linear_stream_kernel");
+}
+template <int NT>
+int launch_stream(const StreamParams& p, int grid, cudaStream_t s) {
+  return grid == 16 ? launch_stream<NT, 16>(p, s) : (grid == 8 ? launch_stream<NT, 8>(p, s) : launch_stream<NT, 1>(p, s));
+}
+
+}  // namespace
+
+// Whether the tokens' codes fit beside the rings (of 1280-byte steps, the larger ones).
+bool linear_stream_fits(const LinearArgs& a) {
+  const int steps = (a.C + 63) / 64;
+  return a.M <= kStreamTokens && kSWarps * kSDepth * 1280 + 512 * 4 + (long long)a.M * staged_pitch(steps) <= kSSmem;
+}
+
+int launch_linear_stream(const LinearArgs& a) {
+  StreamParams p{};
+  p.M = a.M; p.C = a.C; p.K = a.K;
+  p.steps = (a.C + 63) / 64;
+  p.tiles = (a.K + 15) / 16;
+  p.pitch = staged_pitch(p.steps);
+  p.ldx = a.ldx; p.ldw = a.ldw; p.ldy = a.ldy;
+  p.x = a.x; p.x_scale = a.x_scale; p.w = a.w; p.w_scale = a.w_scale; p.bias = a.bias; p.y = a.y;
+  p.x_type = a.x_type; p.y_type = a.y_type;
+  p.x_vec = aligned16(a.x) && a.ldx * (long long)type_bytes(a.x_type) % 16 == 0;
+  const int grid = row_grid(a.w, a.ldw);
+  if (a.M <= 8) return launch_stream<1>(p, grid, a.stream);
+  if (a.M <= 16) return launch_stream<2>(p, grid, a.stream);
+  return launch_stream<4>(p, grid, a.stream);
+}
+
+}  // namespace q8

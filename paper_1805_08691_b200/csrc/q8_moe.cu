@@ -27,7 +27,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "q8_token_common.cuh"
+#include "q8_token_ring.cuh"
 
 namespace q8 {
 namespace {
@@ -281,81 +281,6 @@ __device__ __noinline__ bool wait_counted(const unsigned* counter, unsigned n, v
   }
 }
 
-__device__ __forceinline__ void copy_async_16(void* shared, const void* global) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(global) : "memory");
-}
-
-// The rows of an item that this lane copies, from its present step on, and the bytes left of them.
-struct Rows {
-  const signed char *a, *b;
-  int left;
-};
-
-// A warp's ring.  kGrid: 16 or 8, the alignment of every row, or 1: rows anywhere, copied as aligned words each of which holds
-// a byte of the row and put together when they are read.
-template <int kGrid, int kDepth>
-struct Ring {
-  // (depths are chosen so that `room` in MoeShared holds a step of every token's digits, 192 T bytes, within all limits)
-  static constexpr int kStep = kGrid == 1 ? 1280 : 1024, kHalf = kStep / 2, kBytes = kDepth * kStep;
-  const unsigned char* at;  // this lane's bytes of slot 0
-  uint32_t to;
-  int in, out;              // bytes from there to the slots of the next step copied and used
-  int flying;               // steps between them
-  __device__ __forceinline__ void init(const unsigned char* ring, int lane) {
-    at = ring + (kGrid == 1 ? 4 : 16) * lane;
-    to = (uint32_t)__cvta_generic_to_shared(at);
-    in = out = flying = 0;
-  }
-  template <int kBytes>
-  static __device__ __forceinline__ void copy(uint32_t dst, const void* src, bool live) {
-    const int n = live ? kBytes : 0;  // none: zeros
-    if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(kBytes), "r"(n) : "memory");
-  }
-  static __device__ __forceinline__ void copy_row(uint32_t dst, const signed char* row, int left) {
-    if constexpr (kGrid == 16) {
-      copy<16>(dst, row, left > 0);
-    } else if constexpr (kGrid == 8) {
-      copy<8>(dst, row, left > 0);
-      copy<8>(dst + 8, row + 8, left > 8);
-    } else {
-      const int m = (int)((unsigned long long)row & 3ull);
-#pragma unroll
-      for (int k = 0; k < 5; ++k) copy<4>(dst + 128 * k, row - m + 4 * k, 4 * k - m < left && (k < 4 || m > 0));
-    }
-  }
-  static __device__ __forceinline__ uint4 read_row(const unsigned char* src, const signed char* row) {
-    if constexpr (kGrid != 1) {
-      return *reinterpret_cast<const uint4*>(src);
-    } else {
-      const int m = 8 * (int)((unsigned long long)row & 3ull);
-      unsigned u[5];
-#pragma unroll
-      for (int k = 0; k < 5; ++k) u[k] = *reinterpret_cast<const unsigned*>(src + 128 * k);
-      return make_uint4(__funnelshift_r(u[0], u[1], m), __funnelshift_r(u[1], u[2], m), __funnelshift_r(u[2], u[3], m), __funnelshift_r(u[3], u[4], m));
-    }
-  }
-  __device__ __forceinline__ void put(Rows& r) {
-    copy_row(to + in, r.a, r.left);
-    copy_row(to + in + kHalf, r.b, r.left);
-    r.a += 64;
-    r.b += 64;
-    r.left -= 64;
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    in = in == (kDepth - 1) * kStep ? 0 : in + kStep;
-    ++flying;
-  }
-  __device__ __forceinline__ void get(const Rows& r, uint4& a, uint4& b) {
-    // a group for each step: with a full ring the oldest is done when all but the others are
-    if (flying == kDepth) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
-    else asm volatile("cp.async.wait_group 0;" ::: "memory");
-    --flying;
-    a = read_row(at + out, r.a);
-    b = read_row(at + out + kHalf, r.b);
-    out = out == (kDepth - 1) * kStep ? 0 : out + kStep;
-  }
-};
-
 __device__ __forceinline__ float4 load_h4(const MoeParams& p, int row, int i) {
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
   if (i < p.I) v = __ldcg(reinterpret_cast<const float4*>(p.h + (size_t)row * p.h_pitch + i));
@@ -511,9 +436,6 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
     if (gtid == 0) s_next[group] = items;
   }
 }
-
-// Pitch of rows of digits in shared memory: neighbouring rows in different halves of the banks.
-__host__ __device__ __forceinline__ int staged_pitch(int steps) { return steps * 64 + (steps & 1 ? 0 : 64); }
 
 // Shared memory of a block: lists of rows; partial sums of warps that share items; then the warps' rings and digits, the tokens'
 // in phase one if there is room, a warp's own in phase two.  The logits' keys [T][E] lie over sums and rings until the choice
@@ -905,8 +827,6 @@ int warps_per_item(double items, int steps) {
   }
   return best;
 }
-
-int row_grid(const void* w, int len) { return aligned16(w) && len % 16 == 0 ? 16 : (aligned_to(w, 8) && len % 8 == 0 ? 8 : 1); }
 
 template <int NT, int kGrid>
 int launch_experts(MoeParams p, cudaStream_t s) {
