@@ -24,39 +24,73 @@ int validate_linear(const q8_linear_desc* d, LinearArgs* a) {
   return Q8_OK;
 }
 
-// Rows of bytes onto the 16-byte grid: thread = 16 bytes.
+// Rows of bytes onto the 16-byte grid, zeros behind their ends: thread = 16 bytes, from aligned words each of which holds a
+// byte of the row.
 __global__ void __launch_bounds__(256) regrid_kernel(const signed char* __restrict__ in, long long rows, int C, long long ld, signed char* __restrict__ out,
                                                      int pitch) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int chunks = pitch >> 4;
   const long long n = rows * chunks;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
     const long long r = i / chunks;
-    const int c = (int)(i - r * chunks) * 16;
-    *reinterpret_cast<uint4*>(out + r * pitch + c) = load_16<false>(in + r * ld, c, C);
+    const int c = (int)(i - r * chunks) * 16, left = C - c;
+    const unsigned long long at = (unsigned long long)(in + r * ld + c);
+    const unsigned* w = reinterpret_cast<const unsigned*>(at & ~3ull);
+    const int m = (int)(at & 3ull);
+    unsigned u[5], v[4];
+#pragma unroll
+    for (int k = 0; k < 5; ++k) u[k] = 4 * k - m < left && (k < 4 || m > 0) ? __ldg(w + k) : 0u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[k] = __funnelshift_r(u[k], u[k + 1], 8 * m);
+      const int valid = left - 4 * k;
+      if (valid < 4) v[k] &= valid <= 0 ? 0u : (1u << (8 * valid)) - 1u;
+    }
+    *reinterpret_cast<uint4*>(out + r * pitch + c) = make_uint4(v[0], v[1], v[2], v[3]);
   }
 }
 int regrid(const int8_t* in, long long rows, int C, long long ld, int8_t* out, int pitch, cudaStream_t s) {
   const long long blocks = (rows * (pitch >> 4) + 255) / 256, most = (long long)sm_count() * 32;
-  regrid_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, s>>>(in, rows, C, ld, out, pitch);
-  return check_launch("regrid_kernel");
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(blocks < most ? blocks : most));
+  cfg.blockDim = dim3(256);
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return check_cuda(cudaLaunchKernelEx(&cfg, regrid_kernel, in, rows, C, ld, out, pitch), "regrid_kernel");
 }
 
 bool on_grid(const void* p, long long ld) { return aligned16(p) && ld % 16 == 0 && ld < (1ll << 40); }
-bool few_tokens(const LinearArgs& a) { return linear_stream_fits(a); }
-// Floating-point activations of so few tokens are quantized by every block of the streaming kernel.
-constexpr int kStagedTokens = 4;
 size_t up16(size_t v) { return (v + 15) & ~(size_t)15; }
 
-// Parts of the workspace: codes and factors of x, weights on the grid; a part of zero bytes is not needed.
-struct LinearSpace { size_t codes, factors, weights; size_t bytes() const { return codes + factors + weights; } };
-LinearSpace linear_space(const LinearArgs& a, bool x_on_grid, bool w_on_grid) {
-  LinearSpace s{0, 0, 0};
-  const bool few = few_tokens(a);
-  if (a.M == 0 || (few && (a.x_type == Q8_S8 || a.M <= kStagedTokens))) return s;
-  if (a.x_type != Q8_S8) s.factors = up16((size_t)a.M * 4);
-  if (a.x_type != Q8_S8 || !x_on_grid) s.codes = (size_t)a.M * up16(a.C);
-  if (!w_on_grid && !few) s.weights = (size_t)a.K * up16(a.C);
-  return s;
+// The kernel of a call with scratch, by estimated times, and the parts of the scratch: codes and factors of x, weights on the
+// grid (a part of zero bytes is not needed).
+enum LinearKernel { kStream, kSplit, kPairs };
+struct LinearPlan {
+  LinearKernel kernel;
+  size_t codes, factors, weights;
+  size_t bytes() const { return codes + factors + weights; }
+};
+// Floating-point activations of so few tokens are quantized by every block of the streaming kernel (4096 -> 4096: 2 tokens 6.5
+// us, 4 tokens 9.3; with a launch before it 7.9 us for 8).
+constexpr int kStagedTokens = 2;
+
+LinearPlan plan_linear(const LinearArgs& a, bool x_on_grid, bool w_on_grid) {
+  LinearPlan p{kStream, 0, 0, 0};
+  const bool floats = a.x_type != Q8_S8;
+  // what the tensor-core kernels need before them
+  const double before = (floats || !x_on_grid ? 1.5 : 0.0) + (w_on_grid ? 0.0 : 1.5 + 0.5e-6 * a.C * a.K);
+  const double split = linear_split_us(a), pairs = linear_umma_us(a);
+  if (!linear_stream_fits(a) || linear_stream_us(a) + (floats && a.M > kStagedTokens ? 1.5 : 0.0) > (split < pairs ? split : pairs) + before)
+    p.kernel = split < pairs ? kSplit : kPairs;
+  if (floats && (p.kernel != kStream || a.M > kStagedTokens)) p.factors = up16((size_t)a.M * 4);
+  if (p.factors || (p.kernel != kStream && !x_on_grid)) p.codes = (size_t)a.M * up16(a.C);
+  if (p.kernel != kStream && !w_on_grid) p.weights = (size_t)a.K * up16(a.C);
+  return p;
 }
 
 }  // namespace
@@ -72,7 +106,7 @@ int q8_linear_workspace_bytes(const q8_linear_desc* d, size_t* bytes) {
   const int rc = validate_linear(d, &a);
   if (rc != Q8_OK) return rc;
   if (!bytes) return fail(Q8_ERR_INVALID_ARG, "q8_linear_workspace_bytes: null pointer");
-  *bytes = linear_space(a, on_grid(nullptr, a.ldx), on_grid(nullptr, a.ldw)).bytes();
+  *bytes = a.M ? plan_linear(a, on_grid(nullptr, a.ldx), on_grid(nullptr, a.ldw)).bytes() : 0;
   return Q8_OK;
 }
 
@@ -91,13 +125,12 @@ int q8_linear(const q8_linear_desc* d, const void* x, const float* x_scale, cons
   if (a.M == 0) return Q8_OK;
   a.x = x; a.x_scale = x_scale; a.w = w; a.w_scale = w_scale; a.bias = bias; a.y = y;
   a.stream = as_stream(stream);
-  const LinearSpace sp = linear_space(a, on_grid(x, a.ldx), on_grid(w, a.ldw));
-  const bool few = few_tokens(a);
-  if (sp.bytes() > (workspace ? workspace_bytes : 0) || (few && sp.bytes() == 0)) return few ? launch_linear_stream(a) : launch_linear_rows(a);
+  const LinearPlan sp = plan_linear(a, on_grid(x, a.ldx), on_grid(w, a.ldw));
+  if (sp.bytes() > (workspace ? workspace_bytes : 0)) return linear_stream_fits(a) ? launch_linear_stream(a) : launch_linear_rows(a);
   int8_t* const codes = static_cast<int8_t*>(workspace);
   float* const factors = reinterpret_cast<float*>(codes + sp.codes);
   const int pitch = (int)up16(a.C);
-  if (a.x_type != Q8_S8) {
+  if (sp.factors) {
     rc = launch_quantize_tokens(x, a.x_type, (size_t)a.M, (size_t)a.C, (size_t)a.ldx, codes, (size_t)pitch, factors, a.stream);
     a.x_type = Q8_S8; a.x_scale = factors;
   } else if (sp.codes) {
@@ -111,7 +144,7 @@ int q8_linear(const q8_linear_desc* d, const void* x, const float* x_scale, cons
     if (rc != Q8_OK) return rc;
     a.w = weights; a.ldw = pitch;
   }
-  return few ? launch_linear_stream(a) : launch_linear_umma(a);
+  return sp.kernel == kStream ? launch_linear_stream(a) : (sp.kernel == kSplit ? launch_linear_split(a) : launch_linear_umma(a));
 }
 
 }  // extern "C"

@@ -1,0 +1,329 @@
+// The product with a factor per token on the tensor cores, for token counts between those of the streaming kernel and those
+// that fill the GPU with large tiles.
+//
+//   D[128 output channels, BN tokens] (int32, TMEM) = W[128, C] (s8, TMA) x Z[BN, C]^T (s8, TMA)
+//
+// Bound by the latency of one tile's reduction and by the bytes of the weights, so the weights take the side of 128 rows (BN
+// follows the number of tokens) and the reduction is cut into 2, 4 or 8 parts where there are few tiles: a cluster of CTAs,
+// each with a part of C.  Each leaves its int32 partial sums in its shared memory, whose ring of operands is free by then;
+// behind a cluster barrier every CTA adds up a share of the tokens over all parts (distributed shared memory; integers, so the
+// order does not matter), scales and stores it, 64 bytes of a token's row a warp.  The first weights are on their way into L2
+// while the kernel before drains (a hint: what they will be is read later).
+//
+// Roles: warp 0 loads, warp 1 issues tcgen05.mma.cta_group::1.kind::i8 (128 x BN x 32) and owns the TMEM, warps 2 to 9 take
+// the results.  All waits are bounded.
+//
+// 4096 -> 4096, 64 tokens: 7.1 us (13.4 us with tiles of 256 tokens, 13.4 us with 32 of them through the streaming kernel);
+// 2048 -> 5632, 24 tokens: 5.6 us, of which the weights' bytes are 1.8.
+#include <type_traits>
+
+#include "q8_linear.h"
+#include "q8_token_common.cuh"
+#include "q8_linear_maps.cuh"
+
+namespace q8 {
+namespace {
+
+constexpr int kPBK = 128;
+constexpr int kPEpiWarps = 8, kPThreads = 64 + 32 * kPEpiWarps;
+constexpr int kPMaxStages = 8;
+
+struct SplitParams {
+  int M, K;
+  int bn, kblocks, kb, per, parts, stages, tmem_cols;  // kb: blocks of 128 bytes a stage holds and a load brings
+  unsigned stage_bytes, off_x, idesc, desc_hi;         // off_x: the codes' place in a stage
+  const float* x_scale;
+  const float* w_scale;
+  const float* bias;
+  void* y;
+  long long ldy;
+  int y_vec;  // four values of y can be stored at once
+  unsigned* status;
+};
+
+__device__ __forceinline__ int4 load_peer(uint32_t addr) {
+  int4 v;
+  asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kPThreads, 1)
+    linear_split_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ SplitParams p) {
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) unsigned long long full[kPMaxStages], empty[kPMaxStages], acc_full;
+  __shared__ uint32_t tmem_holder;
+  __shared__ int abort_flag;
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  const int part = p.parts == 1 ? 0 : (int)cluster_ctarank();
+  const int n0 = (int)(blockIdx.x / p.parts) * 128, m0 = (int)blockIdx.y * p.bn;
+  const int kb0 = min(p.kblocks, part * p.per), kb1 = min(p.kblocks, kb0 + p.per);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (warp == 0) {
+    if (lane < p.stages) { mbar_init(smem_u32(&full[lane]), 1); mbar_init(smem_u32(&empty[lane]), 1); }
+    else if (lane == 16) { mbar_init(smem_u32(&acc_full), 1); abort_flag = 0; }
+    else if (lane == 17) prefetch_tensormap(&tmX);
+    else if (lane == 18) prefetch_tensormap(&tmW);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    const int first = kb0 + lane * p.kb;
+    if (lane < p.stages && first < kb1) {
+      if (p.kb > 1) asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global [%0, {%1, %2, %3}];" ::"l"(&tmW), "r"(0), "r"(n0), "r"(first) : "memory");
+      else asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(&tmW), "r"(first * kPBK), "r"(n0) : "memory");
+    }
+  } else if (warp == 1) {
+    tmem_alloc(smem_u32(&tmem_holder), (uint32_t)p.tmem_cols);
+    tmem_relinquish();
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  tcgen05_fence_after();
+  const uint32_t tmem = tmem_holder;
+  volatile int* abortp = &abort_flag;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  int issued = 0;
+  if (warp == 0) {
+    uint32_t stage = 0, phase = 1;
+    bool ok = true;
+    for (int kb = kb0; kb < kb1; kb += p.kb) {
+      if (!mbar_wait(smem_u32(&empty[stage]), phase, abortp)) { ok = false; break; }
+      if (elect_one()) {
+        const uint32_t bar = smem_u32(&full[stage]), dst = base + stage * p.stage_bytes;
+        mbar_arrive_expect_tx(bar, p.stage_bytes);
+        if (p.kb > 1) {  // (blocks behind the last one are zeros)
+          tma_load_3d(dst, &tmW, bar, 0, n0, kb);
+          tma_load_3d(dst + p.off_x, &tmX, bar, 0, m0, kb);
+        } else {
+          tma_load_2d(dst, &tmW, bar, kb * kPBK, n0);
+          tma_load_2d(dst + p.off_x, &tmX, bar, kb * kPBK, m0);
+        }
+      }
+      ++issued;
+      if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+    }
+    if (!ok && lane == 0) { abort_flag = 1; atomicOr(p.status, kTimeoutProducer); }
+  } else if (warp == 1) {
+    uint32_t stage = 0, phase = 0;
+    bool ok = true;
+    for (int kb = kb0; kb < kb1; kb += p.kb) {
+      if (!mbar_wait(smem_u32(&full[stage]), phase, abortp)) { ok = false; break; }
+      tcgen05_fence_after();
+      if (elect_one()) {
+        const uint32_t at = base + stage * p.stage_bytes;
+        uint32_t a = kDescLbo | ((at >> 4) & 0x3fffu), b = kDescLbo | (((at + p.off_x) >> 4) & 0x3fffu);
+        const int blocks = min(p.kb, kb1 - kb);
+        for (int j = 0; j < blocks; ++j, a += 128u * kPBK >> 4, b += (uint32_t)p.bn * kPBK >> 4)
+          umma_i8_block(tmem, a, b, p.desc_hi, p.idesc, kb + j > kb0 ? 1u : 0u, 4);
+        umma_commit(smem_u32(&empty[stage]));
+      }
+      if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+    }
+    if (ok && elect_one()) umma_commit(smem_u32(&acc_full));
+    if (!ok && lane == 0) { abort_flag = 1; atomicOr(p.status, kTimeoutMma); }
+  }
+  // results: warps 2 to 9, thread = output channel, the two groups of four warps take half of the tokens each
+  const int e = warp - 2, quad = warp & 3, group = e >> 2;
+  const int row = quad * 32 + lane, n = n0 + row;
+  const int chunks = p.bn >> 4, half = (chunks + 1) >> 1, c0 = group * half, c1 = min(chunks, c0 + half);
+  const int tokens = min(p.bn, p.M - m0);
+  const bool live = warp >= 2 && n < p.K;
+  const float ws = live ? __ldg(p.w_scale + n) : 0.0f, bias = live && p.bias ? __ldg(p.bias + n) : 0.0f;
+  int* const sums = reinterpret_cast<int*>(smem_raw + (base - raw));  // [token][128], over the ring
+  auto value = [&](int acc, float xs) {
+    float v = __fmul_rn(__fmul_rn(__int2float_rn(acc), xs), ws);
+    if (p.bias) v = __fadd_rn(v, bias);
+    return from_f32<T>(v);
+  };
+  if (warp >= 2) {
+    bool ok = true;
+    if (kb0 < kb1) {
+      ok = mbar_wait(smem_u32(&acc_full), 0, abortp);
+      if (!ok && lane == 0) { abort_flag = 1; atomicOr(p.status, kTimeoutEpilogue); }
+      tcgen05_fence_after();
+    }
+    if (ok) {
+      const uint32_t t = tmem + ((uint32_t)quad << 21);
+      T* y = static_cast<T*>(p.y) + (long long)m0 * p.ldy + n;
+      for (int c = c0; c < c1; ++c) {
+        int v[16];
+        if (kb0 < kb1) {
+          tmem_ld_16(t + c * 16, v);
+          tmem_ld_wait(v);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = 0;
+        }
+        if (p.parts > 1) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) sums[(c * 16 + j) * 128 + row] = v[j];
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int m = c * 16 + j;
+            if (live && m < tokens) y[(long long)m * p.ldy] = value(v[j], __ldg(p.x_scale + m0 + m));
+          }
+        }
+      }
+    }
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  // After a wait that gave up, loads may still be on their way into this CTA's shared memory.
+  if (warp == 0 && *abortp) {
+    int never = 0;
+    for (int i = max(0, issued - p.stages); i < issued; ++i)
+      mbar_wait_slow(smem_u32(&full[i % p.stages]), (uint32_t)(i / p.stages) & 1u, &never, 100000000ull);
+  }
+  __syncwarp();
+  if (warp == 1) {
+    tcgen05_fence_after();
+    tmem_dealloc(tmem, (uint32_t)p.tmem_cols);
+  }
+  if (p.parts > 1) {
+    cluster_sync_all();
+    if (warp >= 2) {
+      // this CTA's tokens: part, part + parts, ...; a warp takes every eighth of them, a lane four channels.  Two tokens at a
+      // time, up to sixteen loads from the peers in flight
+      const int nn = n0 + 4 * lane, there = min(4, p.K - nn);
+      float wsn[4], bn[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        wsn[j] = j < there ? __ldg(p.w_scale + nn + j) : 0.0f;
+        bn[j] = j < there && p.bias ? __ldg(p.bias + nn + j) : 0.0f;
+      }
+      uint32_t peer[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) peer[q] = q < p.parts ? map_to_cta(base + (uint32_t)lane * 16u, (uint32_t)q) : 0u;
+      T* y = static_cast<T*>(p.y) + (long long)m0 * p.ldy + nn;
+      const int step = p.parts * kPEpiWarps;
+      for (int m = part + p.parts * e; m < tokens; m += 2 * step) {
+        int4 v[2][8];
+        float xs[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int mu = m + u * step;
+          xs[u] = mu < tokens ? __ldg(p.x_scale + m0 + mu) : 0.0f;
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            v[u][q] = make_int4(0, 0, 0, 0);
+            if (q < p.parts && mu < tokens) v[u][q] = load_peer(peer[q] + (uint32_t)mu * 512u);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int mu = m + u * step;
+          if (mu >= tokens) continue;
+          int sum[4] = {0, 0, 0, 0};
+#pragma unroll
+          for (int q = 0; q < 8; ++q) { sum[0] += v[u][q].x; sum[1] += v[u][q].y; sum[2] += v[u][q].z; sum[3] += v[u][q].w; }
+          float f[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            f[j] = __fmul_rn(__fmul_rn(__int2float_rn(sum[j]), xs[u]), wsn[j]);
+            if (p.bias) f[j] = __fadd_rn(f[j], bn[j]);
+          }
+          T* to = y + (long long)mu * p.ldy;
+          if (p.y_vec && there == 4) {
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = make_float4(f[0], f[1], f[2], f[3]);
+            else *reinterpret_cast<uint2*>(to) = make_uint2(pack_two<T>(f[0], f[1]), pack_two<T>(f[2], f[3]));
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (j < there) to[j] = from_f32<T>(f[j]);
+          }
+        }
+      }
+    }
+    __syncwarp();
+    cluster_sync_all();  // the sums are read by the peers
+  }
+}
+
+template <typename T>
+int launch_split(const CUtensorMap& tmX, const CUtensorMap& tmW, const SplitParams& p, dim3 grid, size_t dyn, cudaStream_t s) {
+  static std::atomic<bool> set[kMaxDevices];
+  const int dev = current_device();
+  if (dev < 0 || !set[dev].load(std::memory_order_relaxed)) {
+    const int rc = check_cuda(cudaFuncSetAttribute(linear_split_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit - 2048), "linear_split_kernel");
+    if (rc != Q8_OK) return rc;
+    if (dev >= 0) set[dev].store(true, std::memory_order_relaxed);
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(kPThreads);
+  cfg.dynamicSmemBytes = dyn;
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)p.parts;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = p.parts > 1 ? 2 : 1;
+  return check_cuda(cudaLaunchKernelEx(&cfg, linear_split_kernel<T>, tmX, tmW, p), "linear_split_kernel");
+}
+
+void split_shape(const LinearArgs& a, int* m_tiles, int* n_tiles, int* bn, int* parts) {
+  const int kblocks = (a.C + kPBK - 1) / kPBK;
+  *m_tiles = (int)(((long long)a.M + 255) / 256);
+  *n_tiles = (int)(((long long)a.K + 127) / 128);
+  *bn = (int)(((a.M + *m_tiles - 1) / *m_tiles + 15) & ~15);
+  *parts = 1;
+  while (*parts < 8 && (long long)*m_tiles * *n_tiles * *parts * 2 <= sm_count() && kblocks >= 2 * *parts) *parts *= 2;
+}
+
+}  // namespace
+
+// 4096 -> 4096: 16 tokens 6.0 us, 64 7.1, 128 8.5, 256 11.7; 2048 -> 5632, 24 tokens: 5.6; 1024 -> 1024, 64 tokens: 5.4;
+// 4096 -> 11008, 8 tokens: 11.2.
+double linear_split_us(const LinearArgs& a) {
+  if (a.M > 256) return 1e30;  // weights read twice: never the fastest (512 tokens 14.8 us, with tiles of 256 tokens 10.9)
+  int m_tiles, n_tiles, bn, parts;
+  split_shape(a, &m_tiles, &n_tiles, &bn, &parts);
+  const int kblocks = (a.C + kPBK - 1) / kPBK, per = (kblocks + parts - 1) / parts;
+  const long long rounds = ((long long)m_tiles * n_tiles * parts + sm_count() - 1) / sm_count();
+  return 3.2 + rounds * (0.25 * per + (parts > 1 ? 0.025 : 0.012) * bn);
+}
+
+int launch_linear_split(const LinearArgs& a) {
+  SplitParams p{};
+  p.M = a.M; p.K = a.K;
+  p.kblocks = (a.C + kPBK - 1) / kPBK;
+  int m_tiles, n_tiles;
+  split_shape(a, &m_tiles, &n_tiles, &p.bn, &p.parts);
+  p.kb = blocks_per_load(a.C);
+  p.per = (p.kblocks + p.parts - 1) / p.parts;
+  p.per = (p.per + p.kb - 1) / p.kb * p.kb;
+  p.off_x = (unsigned)(p.kb * 128) * kPBK;
+  p.stage_bytes = (unsigned)(p.kb * (128 + p.bn)) * kPBK;
+  int stages = (int)((kSmemLimit - 2048 - 1024) / p.stage_bytes);
+  if (stages > kPMaxStages) stages = kPMaxStages;
+  if (stages > p.per / p.kb) stages = p.per / p.kb;
+  p.stages = stages;
+  size_t dyn = (size_t)p.stages * p.stage_bytes;
+  if (p.parts > 1 && dyn < (size_t)p.bn * 512) dyn = (size_t)p.bn * 512;
+  dyn += 1024;
+  if (dyn < 116 * 1024) dyn = 116 * 1024;  // one CTA an SM, with all of its TMEM to allocate from
+  p.tmem_cols = 32;
+  while (p.tmem_cols < p.bn) p.tmem_cols *= 2;
+  p.idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((unsigned)(p.bn >> 3) << 17) | ((128u >> 4) << 24);
+  p.desc_hi = (unsigned)((8 * kPBK) >> 4) | (1u << 14) | (2u << 29);
+  p.x_scale = a.x_scale; p.w_scale = a.w_scale; p.bias = a.bias;
+  p.y = a.y; p.ldy = a.ldy;
+  p.y_vec = aligned_to(a.y, 4 * type_bytes(a.y_type)) && a.ldy % 4 == 0;
+  p.status = status_word_device_ptr();
+  if (!p.status) return fail(Q8_ERR_CUDA, "linear_split: status word not available");
+  CUtensorMap tmX, tmW;
+  int rc = encode_blocks(&tmX, a.x, a.ldx, a.C, a.M, p.bn, p.kb);
+  if (rc == Q8_OK) rc = encode_blocks(&tmW, a.w, a.ldw, a.C, a.K, 128, p.kb);
+  if (rc != Q8_OK) return rc;
+  const dim3 grid((unsigned)(n_tiles * p.parts), (unsigned)m_tiles);
+  if (a.y_type == Q8_F32) return launch_split<float>(tmX, tmW, p, grid, dyn, a.stream);
+  if (a.y_type == Q8_F16) return launch_split<__half>(tmX, tmW, p, grid, dyn, a.stream);
+  return launch_split<__nv_bfloat16>(tmX, tmW, p, grid, dyn, a.stream);
+}
+
+}  // namespace q8

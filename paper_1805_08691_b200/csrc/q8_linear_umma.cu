@@ -9,26 +9,27 @@
 //
 // Roles of a CTA: warp 0 loads, warp 1 issues (leader) and owns the TMEM, warps 2 to 9 scale and store: thread = accumulator
 // row (token), the two groups of four warps take half of the columns each.  All waits are bounded.
+#include <cmath>
 #include <type_traits>
 
 #include "q8_linear.h"
 #include "q8_token_common.cuh"
-#include "q8_umma_common.cuh"
+#include "q8_linear_maps.cuh"
 
 namespace q8 {
 namespace {
 
-constexpr int kLBK = 128;                      // bytes of the reduction per stage
+constexpr int kLBK = 128;                      // bytes of the reduction per block
 constexpr int kLEpiWarps = 8, kLThreads = 64 + 32 * kLEpiWarps;
 constexpr int kLMaxStages = 8;
 constexpr unsigned kLABytes = 128 * kLBK;
 
 struct LinearParams {
   int M, K;
-  int bn, kblocks, stages, m_tiles, n_tiles;
+  int bn, kblocks, kb, stages, m_tiles, n_tiles;  // kb: blocks of 128 bytes a stage holds and a load brings
   FastDiv fd_group, fd_rows;  // see tile_of
   int group;
-  unsigned stage_bytes, idesc, desc_hi;
+  unsigned stage_bytes, off_w, idesc, desc_hi;   // off_w: the weights' place in a stage
   const float* x_scale;
   const float* w_scale;
   const float* bias;
@@ -124,13 +125,18 @@ __global__ void __launch_bounds__(kLThreads, 1) __cluster_dims__(2, 1, 1)
       int mt, nt;
       tile_of(p, tile, &mt, &nt);
       const int m0 = mt * 256 + rank * 128, n0 = nt * p.bn + rank * half;
-      for (int kb = 0; kb < p.kblocks; ++kb) {
+      for (int kb = 0; kb < p.kblocks; kb += p.kb) {
         if (!mbar_wait(smem_u32(&empty[stage]), phase, abortp)) { ok = false; break; }
         if (elect_one()) {
           const uint32_t bar = smem_u32(&full[stage]), lbar = map_to_cta(bar, 0), dst = base + stage * p.stage_bytes;
           if (rank == 0) mbar_arrive_expect_tx(bar, 2u * p.stage_bytes);
-          tma_load_2d_pair(dst, &tmX, lbar, kb * kLBK, m0);
-          tma_load_2d_pair(dst + kLABytes, &tmW, lbar, kb * kLBK, n0);
+          if (p.kb > 1) {  // (blocks behind the last one are zeros)
+            tma_load_3d_pair(dst, &tmX, lbar, 0, m0, kb);
+            tma_load_3d_pair(dst + p.off_w, &tmW, lbar, 0, n0, kb);
+          } else {
+            tma_load_2d_pair(dst, &tmX, lbar, kb * kLBK, m0);
+            tma_load_2d_pair(dst + p.off_w, &tmW, lbar, kb * kLBK, n0);
+          }
         }
         ++issued;
         if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
@@ -139,22 +145,26 @@ __global__ void __launch_bounds__(kLThreads, 1) __cluster_dims__(2, 1, 1)
     if (!ok && lane == 0) { abort_flag = 1; atomicOr(p.status, kTimeoutProducer); }
   } else if (warp == 1) {
     if (rank == 0) {
+      const uint32_t w16 = (uint32_t)half * kLBK >> 4;
       uint32_t stage = 0, phase = 0, ab = 0, apar = 1;
       bool ok = true;
       for (int tile = first; tile < tiles && ok; tile += step) {
         if (!mbar_wait(smem_u32(&acc_empty[ab]), apar, abortp)) { ok = false; break; }
         tcgen05_fence_after();
         const uint32_t d = tmem + ab * 256u;
-        for (int kb = 0; kb < p.kblocks; ++kb) {
+        for (int kb = 0; kb < p.kblocks; kb += p.kb) {
           if (!mbar_wait(smem_u32(&full[stage]), phase, abortp)) { ok = false; break; }
           tcgen05_fence_after();
           if (elect_one()) {
             const uint32_t at = base + stage * p.stage_bytes;
-            const uint32_t a = kDescLbo | ((at >> 4) & 0x3fffu), b = kDescLbo | (((at + kLABytes) >> 4) & 0x3fffu);
-            umma_i8_pair(d, a, b, p.desc_hi, p.idesc, kb ? 1u : 0u);
-            umma_i8_pair(d, a + 2, b + 2, p.desc_hi, p.idesc, 1u);
-            umma_i8_pair(d, a + 4, b + 4, p.desc_hi, p.idesc, 1u);
-            umma_i8_pair(d, a + 6, b + 6, p.desc_hi, p.idesc, 1u);
+            uint32_t a = kDescLbo | ((at >> 4) & 0x3fffu), b = kDescLbo | (((at + p.off_w) >> 4) & 0x3fffu);
+            const int n = min(p.kb, p.kblocks - kb);
+            for (int j = 0; j < n; ++j, a += kLABytes >> 4, b += w16) {
+              umma_i8_pair(d, a, b, p.desc_hi, p.idesc, kb + j ? 1u : 0u);
+              umma_i8_pair(d, a + 2, b + 2, p.desc_hi, p.idesc, 1u);
+              umma_i8_pair(d, a + 4, b + 4, p.desc_hi, p.idesc, 1u);
+              umma_i8_pair(d, a + 6, b + 6, p.desc_hi, p.idesc, 1u);
+            }
             umma_commit_pair(smem_u32(&empty[stage]));
           }
           if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
@@ -242,17 +252,6 @@ __global__ void __launch_bounds__(kLThreads, 1) __cluster_dims__(2, 1, 1)
   }
 }
 
-int encode_rows_map(CUtensorMap* map, const void* base, long long ld, int C, long long rows, int box_rows) {
-  const DriverFns& fn = driver_fns();
-  if (!fn.tiled) return fail(Q8_ERR_CUDA, "linear_umma: cuTensorMapEncodeTiled entry point not available");
-  cuuint64_t dims[2] = {(cuuint64_t)C, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
-  cuuint32_t box[2] = {(cuuint32_t)kLBK, (cuuint32_t)box_rows}, ones[2] = {1, 1};
-  const CUresult r = fn.tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return fail(Q8_ERR_CUDA, "linear_umma: tensor map rejected (CUresult %d)", (int)r);
-  return Q8_OK;
-}
-
 template <typename T>
 int launch_pairs(const CUtensorMap& tmX, const CUtensorMap& tmW, const LinearParams& p, int grid, size_t dyn, cudaStream_t s) {
   static std::atomic<bool> set[kMaxDevices];
@@ -275,20 +274,48 @@ int launch_pairs(const CUtensorMap& tmX, const CUtensorMap& tmW, const LinearPar
   return check_cuda(cudaLaunchKernelEx(&cfg, linear_umma_kernel<T>, tmX, tmW, p), "linear_umma_kernel");
 }
 
+// Output channels of a tile, and the estimated time: per 128 bytes of the reduction, and for the results behind the last.
+// 4096 -> 4096, 256 tokens: 64 channels 9.3 us, 128 10.0, 256 15.4; 512 tokens: 14.5, 10.9, 15.8; 4096 tokens: 79, 53.5, 46.6.
+int pair_shape(const LinearArgs& a, double* us) {
+  constexpr int kWidth[4] = {64, 96, 128, 256};
+  constexpr double kBlock[4] = {0.17, 0.18, 0.20, 0.34}, kEnd[4] = {1.0, 1.3, 1.6, 2.8};
+  const double kblocks = (a.C + kLBK - 1) / kLBK, pairs = sm_count() / 2;
+  const long long m_tiles = ((long long)a.M + 255) / 256;
+  int best = 0;
+  double least = 1e30;
+  for (int i = 0; i < 4; ++i) {
+    const long long tiles = m_tiles * ((a.K + kWidth[i] - 1) / kWidth[i]);
+    const double rounds = ceil(tiles / pairs), tile = kblocks * kBlock[i] > kEnd[i] ? kblocks * kBlock[i] : kEnd[i];
+    const double t = 2.2 + rounds * tile + kEnd[i];
+    if (t < least) { least = t; best = i; }
+  }
+  if (us) *us = least;
+  return kWidth[best];
+}
+
 }  // namespace
+
+double linear_umma_us(const LinearArgs& a) {
+  double us;
+  pair_shape(a, &us);
+  return us;
+}
 
 int launch_linear_umma(const LinearArgs& a) {
   LinearParams p{};
   p.M = a.M; p.K = a.K;
   p.kblocks = (a.C + kLBK - 1) / kLBK;
   p.m_tiles = (int)(((long long)a.M + 255) / 256);
-  p.bn = 256;
+  p.bn = pair_shape(a, nullptr);
   p.n_tiles = (a.K + p.bn - 1) / p.bn;
   p.group = p.m_tiles < 8 ? p.m_tiles : 8;
   p.fd_group = make_fastdiv(p.group * p.n_tiles);
   p.fd_rows = make_fastdiv(p.group);
-  p.stage_bytes = kLABytes + (unsigned)(p.bn / 2) * kLBK;
-  p.stages = 6;
+  p.kb = p.bn <= 128 ? blocks_per_load(a.C) : 1;  // (wide tiles are long enough: 46.6 us with one block, 48.2 with two)
+  p.off_w = (unsigned)p.kb * kLABytes;
+  p.stage_bytes = p.off_w + (unsigned)(p.kb * (p.bn / 2)) * kLBK;
+  p.stages = (int)((kSmemLimit - 8192 - 1024) / p.stage_bytes);
+  if (p.stages > kLMaxStages) p.stages = kLMaxStages;
   p.idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((unsigned)(p.bn >> 3) << 17) | ((256u >> 4) << 24);
   p.desc_hi = (unsigned)((8 * kLBK) >> 4) | (1u << 14) | (2u << 29);
   p.x_scale = a.x_scale; p.w_scale = a.w_scale; p.bias = a.bias;
@@ -297,8 +324,8 @@ int launch_linear_umma(const LinearArgs& a) {
   p.status = status_word_device_ptr();
   if (!p.status) return fail(Q8_ERR_CUDA, "linear_umma: status word not available");
   CUtensorMap tmX, tmW;
-  int rc = encode_rows_map(&tmX, a.x, a.ldx, a.C, a.M, 128);
-  if (rc == Q8_OK) rc = encode_rows_map(&tmW, a.w, a.ldw, a.C, a.K, p.bn / 2);
+  int rc = encode_blocks(&tmX, a.x, a.ldx, a.C, a.M, 128, p.kb);
+  if (rc == Q8_OK) rc = encode_blocks(&tmW, a.w, a.ldw, a.C, a.K, p.bn / 2, p.kb);
   if (rc != Q8_OK) return rc;
   const long long tiles = (long long)p.m_tiles * p.n_tiles, pairs = sm_count() / 2;
   const int grid = 2 * (int)(tiles < pairs ? tiles : pairs);
