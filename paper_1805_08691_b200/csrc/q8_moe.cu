@@ -3,7 +3,7 @@
 // Few tokens read each chosen expert's weights once and do little else: the layer is bound by the bytes of the weights, and
 // everything between two streams of them is latency.  Two kernels:
 //
-//   moe_route_kernel    logits in 64 bits, a warp per (token, expert); the tokens as integer digits, a block per token;
+//   moe_route_kernel    logits in 64 bits, a block per expert and four tokens; the tokens as integer digits, a block each;
 //   moe_experts_kernel  all the rest.  Every block finds the chosen experts itself.  Then warps draw items by tickets: first
 //                       of eight inner units (their eight gate and eight up rows are the sixteen rows of an instruction),
 //                       then of sixteen output channels of an expert.
@@ -20,9 +20,10 @@
 // also waited for the weights issued before it; 16 tokens, 64 experts 124 us.)
 //
 // What phase two reads of phase one: the largest magnitudes of the rows of inner activations are collected while these are
-// made; behind the last item of phase one, warps draw rows, wait for the items of the row's expert and turn it into digits.
-// A warp waits for an expert's rows only with its first down weights already on their way, and with every item it waits for
-// in the hands of a running warp: progress needs no co-residency.  Waits are bounded all the same.
+// made; behind the last item of phase one, warps draw rows and turn them into digits (with few of them every reader does so
+// itself).  A warp counts its items once, at the end of a phase: a fence for each item would wait for the copies on their way
+// too.  A warp waits with its first down weights on their way, and with every item it waits for in the hands of a running
+// warp: progress needs no co-residency.  Waits are bounded all the same.
 #include <atomic>
 #include <cmath>
 #include <type_traits>
@@ -34,14 +35,19 @@ namespace {
 
 constexpr int kMoeGroup = 16;    // tokens of a pass
 constexpr int kMoeRows = 256;    // ... times top_k, at most
-constexpr int kMoeWarps = 16, kMoeThreads = 32 * kMoeWarps;
 constexpr int kMaxTopK = 32;      // a lane each
 constexpr int kMaxExperts = 1024; // a bit of a lane's word each
-constexpr int kDepth1 = 5;       // steps of 16 x 64 bytes in a warp's ring: 80 KiB of weights on their way to an SM
-constexpr int kDepth2 = 5;       // ... in phase two
-constexpr int kDepth2Odd = 5;    // ... where a step takes 1280 bytes
+// Warps of a block, by the eights of columns of its kernel: with many columns a warp needs more than 128 registers.
+__host__ __device__ constexpr int warps_of(int nt) { return nt > 2 ? 8 : 16; }
+// Steps of 16 x 64 bytes in a warp's ring: 80 KiB of weights on their way to an SM in phase one, 128 KiB in phase two, whose
+// items are shorter and have more to wait for.  (kGrid 1: a step takes 1280 bytes.  The depths are chosen so that `room` in
+// MoeShared holds a step of every token's digits, 192 T bytes, within all limits.)
+__host__ __device__ constexpr int depth1_of(int nt) { return 80 / warps_of(nt); }
+__host__ __device__ constexpr int depth2_of(int nt, int step_bytes) { return (step_bytes == 1024 ? 128 : 96) / warps_of(nt); }
 constexpr float kDigitMax = 8355711.0f;  // 127 (256^2 + 256 + 1)
-constexpr int kTickets = 6;
+// Tickets: blocks and items of phase one, of phase two, rows to be made digits, tiles to be added up; then how many items of
+// phase one, rows and items of phase two are done.
+enum { kBlocks1, kItems1, kBlocks2, kItems2, kRows, kTiles, kDone1, kDoneRows, kDone2, kCounters };
 constexpr int kDirectSteps = 32; // tokens times steps up to which the readers of inner activations make their digits themselves
 constexpr unsigned kTimeoutMoe = 32u;
 constexpr unsigned long long kMoeWaitNs = 2000000000ull;
@@ -67,8 +73,7 @@ struct MoeParams {
   // workspace
   double* logits;        // [T][E]
   float* x_factor;       // [T]
-  unsigned* sync;        // tickets (blocks and items of either phase, rows, tiles); per chosen expert the finished items, then the rows made digits; finished items per
-                         // tile; per row its largest magnitude
+  unsigned* sync;        // tickets and counters (kBlocks1 ..), then the largest magnitude of each row
   float* part;           // weighted results of the experts [T k][C]
   signed char* xd;       // digits of the tokens [T][3][x_pitch]
   signed char* hd;       // digits of the inner activations [T k][3][h_pitch]
@@ -140,13 +145,14 @@ __device__ __forceinline__ float digits_sum(int a, int b, int c) {
 }
 
 // ------------------------------------------------------------------------------------------ router
+template <int kTok>
 __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ MoeParams p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if ((int)blockIdx.x < p.T) {  // digits of a token
     const int t = blockIdx.x;
-    if (t == 0) for (int i = threadIdx.x; i < kTickets + 2 * min(p.E, p.T * p.k) + p.tiles + p.T * p.k; i += 256) p.sync[i] = 0u;
+    if (t == 0) for (int i = threadIdx.x; i < kCounters + p.T * p.k; i += 256) p.sync[i] = 0u;
     __shared__ unsigned part[8];
     unsigned m = 0;
     if (p.x_vec) {
@@ -183,49 +189,50 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
     }
     return;
   }
-  // all tokens' logits of an expert; a thread's share of the channels does not depend on their number
-  __shared__ double part_sum[8][kMoeGroup];
-  const int e = (int)blockIdx.x - p.T;
+  // an expert's logits of kTok tokens; a thread's share of the channels does not depend on their number
+  __shared__ double part_sum[8][kTok];
+  const int index = (int)blockIdx.x - p.T, e = index % p.E, t0 = index / p.E * kTok;
   const float* r = p.router + (size_t)e * p.C;
-  double s[kMoeGroup];
+  double s[kTok];
+  int row[kTok];
 #pragma unroll
-  for (int t = 0; t < kMoeGroup; ++t) s[t] = 0.0;
+  for (int t = 0; t < kTok; ++t) { s[t] = 0.0; row[t] = min(t0 + t, p.T - 1); }
   if (p.x_vec && p.r_vec) {
+#pragma unroll 2
     for (int c = 4 * threadIdx.x; c < p.C; c += 1024) {
       const float4 w = __ldg(reinterpret_cast<const float4*>(r + c));
+      float4 v[kTok];
 #pragma unroll
-      for (int t = 0; t < kMoeGroup; ++t) {
-        if (t >= p.T) break;
-        const float4 v = load_x4(p, t, c);
-        s[t] = __fma_rn((double)v.x, (double)w.x, s[t]);
-        s[t] = __fma_rn((double)v.y, (double)w.y, s[t]);
-        s[t] = __fma_rn((double)v.z, (double)w.z, s[t]);
-        s[t] = __fma_rn((double)v.w, (double)w.w, s[t]);
+      for (int t = 0; t < kTok; ++t) v[t] = load_x4(p, row[t], c);
+#pragma unroll
+      for (int t = 0; t < kTok; ++t) {
+        s[t] = __fma_rn((double)v[t].x, (double)w.x, s[t]);
+        s[t] = __fma_rn((double)v[t].y, (double)w.y, s[t]);
+        s[t] = __fma_rn((double)v[t].z, (double)w.z, s[t]);
+        s[t] = __fma_rn((double)v[t].w, (double)w.w, s[t]);
       }
     }
   } else {
+#pragma unroll 2
     for (int c = threadIdx.x; c < p.C; c += 256) {
       const double w = (double)r[c];
 #pragma unroll
-      for (int t = 0; t < kMoeGroup; ++t) {
-        if (t >= p.T) break;
-        s[t] = __fma_rn((double)load_x(p, t, c), w, s[t]);
-      }
+      for (int t = 0; t < kTok; ++t) s[t] = __fma_rn((double)load_x(p, row[t], c), w, s[t]);
     }
   }
 #pragma unroll
-  for (int t = 0; t < kMoeGroup; ++t) {
-    if (t >= p.T) break;
+  for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s[t] += __shfl_xor_sync(0xffffffffu, s[t], o);
+    for (int t = 0; t < kTok; ++t) s[t] += __shfl_xor_sync(0xffffffffu, s[t], o);
+#pragma unroll
+  for (int t = 0; t < kTok; ++t)
     if (lane == 0) part_sum[warp][t] = s[t];
-  }
   __syncthreads();
-  if ((int)threadIdx.x < p.T) {
+  if ((int)threadIdx.x < kTok && t0 + (int)threadIdx.x < p.T) {
     double l = part_sum[0][threadIdx.x];
 #pragma unroll
     for (int w = 1; w < 8; ++w) l += part_sum[w][threadIdx.x];
-    p.logits[(size_t)threadIdx.x * p.E + e] = l;
+    p.logits[(size_t)(t0 + threadIdx.x) * p.E + e] = l;
   }
 }
 
@@ -304,18 +311,18 @@ __device__ __forceinline__ void make_digits(const MoeParams& p, int row, unsigne
 }
 
 // All items of a phase, by groups of ks warps.  J says what an item is: rows() its weights, scales() the factors of this lane's
-// two rows, columns() its digits, finish() takes the sums of a token with these rows (all lanes call it), complete() counts
-// the item as done.
+// two rows, columns() its digits, finish() takes the sums of a token with these rows (all lanes call it).  Behind the last
+// item, `done` has gone up by the items of this call's warps.
 //
 // Block b begins with the items b + blocks * group, and draws those behind them by tickets.  b is drawn too, so that blocks
 // that run have the first numbers; a group that finds no more tickets takes over the first items of a block that has not
 // drawn its number.  Whoever then waits for an item knows it in the hands of a running warp.
 template <int NT, int kGrid, int kDepth, typename J>
-__device__ __forceinline__ void run_phase(const J& job, int items, int steps, int ks, unsigned* tickets, int block, int* s_next, int* acc_all,
+__device__ __forceinline__ void run_phase(const J& job, int items, int steps, int ks, unsigned* tickets, unsigned* done, int block, int* s_next, int* acc_all,
                                           const unsigned char* ring_at, int lane, int warp) {
   const int group = warp / ks, part = warp - group * ks, gtid = part * 32 + lane, threads = 32 * ks, i = lane & 3, g = lane >> 2;
   const int per = (steps + ks - 1) / ks, s0 = min(steps, part * per), n = min(steps, s0 + per) - s0;
-  const int groups = kMoeWarps / ks, blocks = (int)gridDim.x;
+  const int groups = warps_of(NT) / ks, blocks = (int)gridDim.x;
   int* const acc = acc_all + group * (128 * NT) + lane;  // (ks > 1) [4 NT][32]
   auto meet = [&] {
     if (ks == 1) __syncwarp();
@@ -333,6 +340,7 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
   }
   Ring<kGrid, kDepth> ring;
   ring.init(ring_at, lane);
+  unsigned finished = 0;
   for (;;) {
     Rows r = job.rows(cur, items, s0, n, lane), next = r;
     int m = cur < items ? n : 0;  // steps of r not copied yet
@@ -355,29 +363,46 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
         int d[N][4];
 #pragma unroll
         for (int t = 0; t < N; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0;
-        const int chunk = job.prepare(cur, count, n, lane);  // steps whose digits are at hand at a time
-        int c_end = 0;
-#pragma unroll 1
-        for (int s = 0; s < n; ++s) {
-          if (s == c_end) {
-            job.columns(cur, count, s0 + s, min(chunk, n - s), lane, z);
-            c_end += chunk;
-          }
-          uint4 a, b;
-          ring.get(now, a, b);
-#pragma unroll 1
-          do {
-            if (m == 0 && !ahead && nxt < items) { r = next; m = n; ahead = true; }
-            if (m == 0) break;
-            ring.put(r);
-            --m;
-          } while (ring.flying < kDepth);
+        job.columns(cur, count, s0, n, lane, z);
+        // digits a batch of steps ahead: from L2 they take as long as a few steps
+        constexpr int A = N <= 2 ? 4 : (N <= 4 ? 2 : 1);
+        uint4 q[A][N];
+        auto fetch = [&](uint4 (&v)[A][N], int s) {
 #pragma unroll
-          for (int t = 0; t < N; ++t) {
-            const uint4 q = *reinterpret_cast<const uint4*>(z[t]);
-            z[t] += 64;
-            mma_16x8x32(d[t], a.x, b.x, a.y, b.y, q.x, q.y);
-            mma_16x8x32(d[t], a.z, b.z, a.w, b.w, q.z, q.w);
+          for (int j = 0; j < A; ++j)
+#pragma unroll
+            for (int t = 0; t < N; ++t)
+              if (s + j < n) v[j][t] = *reinterpret_cast<const uint4*>(z[t] + 64 * (s + j));
+        };
+        if (N <= 4) fetch(q, 0);
+#pragma unroll 1
+        for (int s = 0; s < n; s += A) {
+          uint4 v[A][N];
+          if (N <= 4) fetch(v, s + A);
+#pragma unroll
+          for (int j = 0; j < A; ++j) {
+            if (s + j >= n) break;
+            uint4 a, b;
+            ring.get(now, a, b);
+#pragma unroll 1
+            do {
+              if (m == 0 && !ahead && nxt < items) { r = next; m = n; ahead = true; }
+              if (m == 0) break;
+              ring.put(r);
+              --m;
+            } while (ring.flying < kDepth);
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+              if (N > 4) q[j][t] = *reinterpret_cast<const uint4*>(z[t] + 64 * (s + j));
+              mma_16x8x32(d[t], a.x, b.x, a.y, b.y, q[j][t].x, q[j][t].y);
+              mma_16x8x32(d[t], a.z, b.z, a.w, b.w, q[j][t].z, q[j][t].w);
+            }
+          }
+          if (N <= 4) {
+#pragma unroll
+            for (int j = 0; j < A; ++j)
+#pragma unroll
+              for (int t = 0; t < N; ++t) q[j][t] = v[j][t];
           }
         }
         if (gtid == 0) s_next[group] = (int)drawn;
@@ -409,12 +434,10 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
         }
       };
       if (NT <= 2 || count <= 4) go(std::integral_constant<int, (NT < 2 ? NT : 2)>{});
+      else if (count <= 8) go(std::integral_constant<int, (NT < 4 ? NT : 4)>{});
       else go(std::integral_constant<int, NT>{});
       if (n == 0 && nxt < items) r = next;
-      if (part == 0) {
-        __syncwarp();
-        job.complete(cur, lane);
-      }
+      ++finished;
       cur = nxt;
     }
     if (gtid == 0) {
@@ -432,8 +455,12 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
     meet();
     cur = s_next[group];
     meet();
-    if (cur >= items) return;
+    if (cur >= items) break;
     if (gtid == 0) s_next[group] = items;
+  }
+  if (part == 0) {
+    __syncwarp();
+    if (lane == 0 && finished) add_release(done, finished);
   }
 }
 
@@ -447,13 +474,13 @@ struct MoeShared {
     rows = T * k;
     chosen = rows < E ? rows : E;
     acc_at = (4 * (7 * rows + 2 * E) + 15) & ~15;
-    rings_at = acc_at + kMoeWarps / 2 * 512 * nt;
-    digits_at = rings_at + kMoeWarps * kDepth1 * step_bytes;
+    rings_at = acc_at + warps_of(nt) / 2 * 512 * nt;
+    digits_at = rings_at + warps_of(nt) * depth1_of(nt) * step_bytes;
     if (digits_at < acc_at + 8 * T * E) digits_at = acc_at + 8 * T * E;
     const int all = 3 * T * staged_pitch(steps);
     staged = all <= kMoeSmem - digits_at;
-    own_at = rings_at + kMoeWarps * (step_bytes == 1024 ? kDepth2 : kDepth2Odd) * step_bytes;
-    room = ((kMoeSmem - own_at) / kMoeWarps) & ~127;
+    own_at = rings_at + warps_of(nt) * depth2_of(nt, step_bytes) * step_bytes;
+    room = ((kMoeSmem - own_at) / warps_of(nt)) & ~127;
     total = kMoeSmem;
   }
 };
@@ -462,7 +489,7 @@ struct MoeShared {
 struct GateUp {
   const MoeParams& p;
   const MoeChoice& ch;
-  unsigned *done, *largest;
+  unsigned* largest;
   const signed char* digits;  // of the tokens, in shared memory or not
   int pitch;
   __device__ __forceinline__ int expert(int item) const { return p.by_unit_blocks(item); }
@@ -477,7 +504,6 @@ struct GateUp {
     r.left = min(p.C, 64 * (s0 + n)) - from;
     return r;
   }
-  __device__ __forceinline__ int prepare(int, int, int n, int) const { return n; }
   template <int NT>
   __device__ __forceinline__ void columns(int item, int count, int s0, int n, int lane, const signed char* (&z)[NT]) const {
     const int first = ch.first[expert(item)], digit = min((lane >> 2) & 3, 2);
@@ -506,23 +532,18 @@ struct GateUp {
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 16));
     if (live && u == 0) atomicMax(&largest[row], m);
   }
-  __device__ __forceinline__ void complete(int item, int lane) const {
-    if (lane == 0) add_release(&done[expert(item)], 1u);
-  }
 };
 
 // Phase two: sixteen output channels of an expert, expert by expert in the order in which phase one completes them.
 struct Down {
   const MoeParams& p;
   const MoeChoice& ch;
-  const unsigned *done, *ready, *largest;
-  unsigned* tile_done;
-  unsigned char* known;
-  int* gave_up;
+  const unsigned* largest;
+  const unsigned* waited;  // a counter and what it has to reach before digits are read
+  unsigned reached;
+  int *known, *gave_up;    // (shared memory) whether a warp of this block has seen it
   signed char* mine;  // shared memory of this warp for an item's digits
-  int room, active;
   __device__ __forceinline__ int expert(int item) const { return p.by_tiles(item); }
-  __device__ __forceinline__ int tile(int item) const { return item - p.by_tiles(item) * p.tiles; }
   __device__ __forceinline__ int count(int item) const { return __popc(ch.tokens[expert(item)]); }
   __device__ __forceinline__ Rows rows(int item, int items, int s0, int n, int lane) const {
     Rows r{p.wd, p.wd, 0};
@@ -534,52 +555,31 @@ struct Down {
     r.left = min(p.I, 64 * (s0 + n)) - from;
     return r;
   }
-  __device__ __forceinline__ int prepare(int item, int count, int n, int lane) const {
-    const int a = expert(item);
-    // (lines of digits belong to one expert: none can be in L1 from before that)
-    if (!__any_sync(0xffffffffu, *reinterpret_cast<volatile unsigned char*>(known + a)) &&
-        (p.direct ? wait_counted(&done[a], (unsigned)p.unit_blocks, gave_up, p.status) : wait_counted(&ready[a], (unsigned)count, gave_up, p.status)))
-      *reinterpret_cast<volatile unsigned char*>(known + a) = 1;
-    __threadfence_block();
-    if (3 * count * staged_pitch(n) <= room) return n;
-    return (room / (192 * count) - 1) | 1;  // (the pitch of an odd number of steps is no longer than they are)
-  }
-  // The digits of n steps from s0 on, in the warp's own shared memory.
   template <int NT>
   __device__ __forceinline__ void columns(int item, int count, int s0, int n, int lane, const signed char* (&z)[NT]) const {
-    const int first = ch.first[expert(item)], pitch = staged_pitch(n), len = 64 * n, digit = min((lane >> 2) & 3, 2);
+    const int a = expert(item), first = ch.first[a], digit = min((lane >> 2) & 3, 2);
+    if (!__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(known)) && wait_counted(waited, reached, gave_up, p.status))
+      *reinterpret_cast<volatile int*>(known) = 1;
+    __threadfence_block();
+    if (!p.direct) {
+      const signed char* from = p.hd + (size_t)first * 3 * p.h_pitch + 64 * s0 + 16 * (lane & 3);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) z[t] = from + (size_t)(min(2 * t + (lane >> 4), count - 1) * 3 + digit) * p.h_pitch;
+      return;
+    }
+    // digits made here, in the warp's own shared memory
+    const int pitch = staged_pitch(n), len = 64 * n;
     __syncwarp();  // (all lanes have read what was there)
-    if (p.direct) {
-      for (int r = 0; r < count; ++r) {
-        const DigitScale scale = digit_scale(__ldcg(largest + first + r));
+    for (int r = 0; r < count; ++r) {
+      const DigitScale scale = digit_scale(__ldcg(largest + first + r));
 #pragma unroll 8
-        for (int c = 4 * lane; c < len; c += 128) {
-          unsigned d0, d1, d2;
-          digits_4(load_h4(p, first + r, 64 * s0 + c), scale, d0, d1, d2);
-          signed char* to = mine + 3 * r * pitch + c;
-          *reinterpret_cast<unsigned*>(to) = d0;
-          *reinterpret_cast<unsigned*>(to + pitch) = d1;
-          *reinterpret_cast<unsigned*>(to + 2 * pitch) = d2;
-        }
-      }
-    } else {
-      const signed char* from = p.hd + (size_t)first * 3 * p.h_pitch + 64 * s0;
-      int r = 0, c = 16 * lane;
-      while (c >= len) { c -= len; ++r; }
-      for (;;) {
-        uint4 v[6];
-        int to[6];
-#pragma unroll
-        for (int j = 0; j < 6; ++j) {
-          to[j] = r < 3 * count ? r * pitch + c : -1;
-          if (to[j] >= 0) v[j] = *reinterpret_cast<const uint4*>(from + (size_t)r * p.h_pitch + c);
-          c += 512;
-          while (c >= len) { c -= len; ++r; }
-        }
-#pragma unroll
-        for (int j = 0; j < 6; ++j)
-          if (to[j] >= 0) *reinterpret_cast<uint4*>(mine + to[j]) = v[j];
-        if (__all_sync(0xffffffffu, r >= 3 * count)) break;
+      for (int c = 4 * lane; c < len; c += 128) {
+        unsigned d0, d1, d2;
+        digits_4(load_h4(p, first + r, 64 * s0 + c), scale, d0, d1, d2);
+        signed char* to = mine + 3 * r * pitch + c;
+        *reinterpret_cast<unsigned*>(to) = d0;
+        *reinterpret_cast<unsigned*>(to + pitch) = d1;
+        *reinterpret_cast<unsigned*>(to + 2 * pitch) = d2;
       }
     }
     __syncwarp();
@@ -599,9 +599,6 @@ struct Down {
     if (c < p.C) out[0] = __fmul_rn(w, __fmul_rn(__fmul_rn(low, f), s.x));
     if (c + 8 < p.C) out[8] = __fmul_rn(w, __fmul_rn(__fmul_rn(high, f), s.y));
   }
-  __device__ __forceinline__ void complete(int item, int lane) const {
-    if (lane == 0) add_release(&tile_done[tile(item)], 1u);
-  }
   // The results of a tile, by a warp.
   __device__ __forceinline__ void add_up(int t, int lane) const {
     const int c = 16 * t + (lane & 15);
@@ -620,9 +617,10 @@ struct Down {
 };
 
 template <int NT, int kGrid>
-__global__ void __launch_bounds__(kMoeThreads, 1) moe_experts_kernel(const __grid_constant__ MoeParams p) {
+__global__ void __launch_bounds__(32 * warps_of(NT), 1) moe_experts_kernel(const __grid_constant__ MoeParams p) {
+  constexpr int kMoeWarps = warps_of(NT), kMoeThreads = 32 * kMoeWarps;
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ int s_active, s_block[2], s_next[kMoeWarps], gave_up;
+  __shared__ int s_active, s_block[2], s_next[kMoeWarps], s_known, gave_up;
   const MoeShared lay(p.T, p.k, p.E, p.steps, Ring<kGrid, 1>::kStep, NT);
   int* const acc = reinterpret_cast<int*>(smem + lay.acc_at);
   unsigned long long* const keys = reinterpret_cast<unsigned long long*>(smem + lay.acc_at);  // [T][E], until the choice is made
@@ -639,11 +637,11 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_experts_kernel(const __gri
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   for (int e = tid; e < p.E; e += kMoeThreads) mask[e] = 0u;
-  if (tid == 0) gave_up = 0;
+  if (tid == 0) s_known = gave_up = 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   signed char* const digits = reinterpret_cast<signed char*>(smem + lay.digits_at);
-  const unsigned char* const ring1 = smem + lay.rings_at + warp * Ring<kGrid, kDepth1>::kBytes;
-  constexpr int kLater = kGrid == 1 ? kDepth2Odd : kDepth2;
+  const unsigned char* const ring1 = smem + lay.rings_at + warp * Ring<kGrid, depth1_of(NT)>::kBytes;
+  constexpr int kLater = depth2_of(NT, Ring<kGrid, 1>::kStep);
   const unsigned char* const ring2 = smem + lay.rings_at + warp * Ring<kGrid, kLater>::kBytes;
   signed char* const own = reinterpret_cast<signed char*>(smem + lay.own_at) + warp * lay.room;
   const int x_staged = staged_pitch(p.steps);
@@ -651,53 +649,67 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_experts_kernel(const __gri
     for (int r = warp; r < 3 * p.T; r += kMoeWarps)
       for (int c = 16 * lane; c < 64 * p.steps; c += 512) copy_async_16(digits + r * x_staged + c, p.xd + (size_t)r * p.x_pitch + c);
   }
-  if (tid < 2) s_block[tid] = (int)atomicAdd(&p.sync[2 * tid], 1u);  // this block's number in either phase
+  if (tid < 2) s_block[tid] = (int)atomicAdd(&p.sync[tid ? kBlocks2 : kBlocks1], 1u);  // this block's number in either phase
   for (int i = tid; i < p.T * p.E; i += kMoeThreads) keys[i] = order_key(__ldcg(p.logits + i));
   __syncthreads();
   // ---- choice: a warp per token
-  const int per_warp = (p.T + kMoeWarps - 1) / kMoeWarps;  // 1 or 2
   int mine[2] = {-1, -1};           // lane j: the j-th chosen expert
   float weight[2] = {0.0f, 0.0f};   // ... its probability
+  constexpr int kBoth = kMoeWarps < kMoeGroup ? 2 : 1;  // tokens of a warp, side by side
+  if (warp < p.T) {
+    const unsigned long long* l[kBoth];
+    unsigned long long key0[kBoth], key_mine[kBoth];
+    unsigned taken[kBoth];  // bit q: expert lane + 32 q
 #pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    const int t = warp + w * kMoeWarps;
-    if (w >= per_warp || t >= p.T) break;
-    const unsigned long long* l = keys + (size_t)t * p.E;
-    unsigned long long key0 = 0ull, key_mine = 0ull;
-    unsigned taken = 0u;  // bit q: expert lane + 32 q
+    for (int w = 0; w < kBoth; ++w) {
+      l[w] = keys + (size_t)min(warp + w * kMoeWarps, p.T - 1) * p.E;
+      key0[w] = key_mine[w] = 0ull;
+      taken[w] = 0u;
+    }
     for (int j = 0; j < p.k; ++j) {
-      unsigned long long key = 0ull;
-      int at = 0x7fffffff;
+      unsigned long long key[kBoth];
+      int at[kBoth];
+#pragma unroll
+      for (int w = 0; w < kBoth; ++w) { key[w] = 0ull; at[w] = 0x7fffffff; }
       for (int q = 0, e = lane; e < p.E; ++q, e += 32) {
-        if (taken >> q & 1u) continue;
-        const unsigned long long o = l[e];
-        if (at == 0x7fffffff || o > key) { key = o; at = e; }
+#pragma unroll
+        for (int w = 0; w < kBoth; ++w) {
+          const unsigned long long o = l[w][e];
+          if (!(taken[w] >> q & 1u) && (at[w] == 0x7fffffff || o > key[w])) { key[w] = o; at[w] = e; }
+        }
       }
       // among lanes that have a candidate, the largest key, then the lowest expert
-      const bool have = at != 0x7fffffff;
-      const unsigned hi = have ? (unsigned)(key >> 32) : 0u;
-      const unsigned top_hi = __reduce_max_sync(0xffffffffu, hi);
-      const bool in = have && hi == top_hi;
-      const unsigned top_lo = __reduce_max_sync(0xffffffffu, in ? (unsigned)key : 0u);
-      const int e = (int)__reduce_min_sync(0xffffffffu, in && (unsigned)key == top_lo ? (unsigned)at : 0x7fffffffu);
-      if ((e & 31) == lane) taken |= 1u << (e >> 5);
-      const unsigned long long top = (unsigned long long)top_hi << 32 | top_lo;
-      if (j == 0) key0 = top;
-      if (lane == j) { mine[w] = e; key_mine = top; }
-    }
-    const double best = key_value(key0);
-    float total = 0.0f;
-    const float ex = lane < p.k ? expf((float)(key_value(key_mine) - best)) : 0.0f;
-    if (p.renormalize) total = ex;
-    else for (int e = lane; e < p.E; e += 32) total += expf((float)(key_value(l[e]) - best));
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    weight[w] = __fdiv_rn(ex, total);
-    if (lane < p.k) {
-      atomicOr(&mask[mine[w]], 1u << t);
-      if (blockIdx.x == 0) {
-        if (p.ids) p.ids[t * p.k + lane] = mine[w];
-        if (p.probs) p.probs[t * p.k + lane] = weight[w];
+      for (int w = 0; w < kBoth; ++w) {
+        const bool have = at[w] != 0x7fffffff;
+        const unsigned hi = have ? (unsigned)(key[w] >> 32) : 0u;
+        const unsigned top_hi = __reduce_max_sync(0xffffffffu, hi);
+        const bool in = have && hi == top_hi;
+        const unsigned top_lo = __reduce_max_sync(0xffffffffu, in ? (unsigned)key[w] : 0u);
+        const int e = (int)__reduce_min_sync(0xffffffffu, in && (unsigned)key[w] == top_lo ? (unsigned)at[w] : 0x7fffffffu);
+        if ((e & 31) == lane) taken[w] |= 1u << (e >> 5);
+        const unsigned long long top = (unsigned long long)top_hi << 32 | top_lo;
+        if (j == 0) key0[w] = top;
+        if (lane == j) { mine[w] = e; key_mine[w] = top; }
+      }
+    }
+#pragma unroll
+    for (int w = 0; w < kBoth; ++w) {
+      const int t = warp + w * kMoeWarps;
+      const double best = key_value(key0[w]);
+      float total = 0.0f;
+      const float ex = lane < p.k ? expf((float)(key_value(key_mine[w]) - best)) : 0.0f;
+      if (p.renormalize) total = ex;
+      else for (int e = lane; e < p.E; e += 32) total += expf((float)(key_value(l[w][e]) - best));
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      weight[w] = __fdiv_rn(ex, total);
+      if (lane < p.k && t < p.T) {
+        atomicOr(&mask[mine[w]], 1u << t);
+        if (blockIdx.x == 0) {
+          if (p.ids) p.ids[t * p.k + lane] = mine[w];
+          if (p.probs) p.probs[t * p.k + lane] = weight[w];
+        }
       }
     }
   }
@@ -724,7 +736,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_experts_kernel(const __gri
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
     const int t = warp + w * kMoeWarps;
-    if (w < per_warp && t < p.T && lane < p.k) {
+    if (w < kBoth && t < p.T && lane < p.k) {
       const int at = index[mine[w]], row = ch.first[at] + __popc(ch.tokens[at] & ((1u << t) - 1u));
       int place = 0;
       for (int j = 0; j < p.k; ++j) place += __shfl_sync(p.k == 32 ? 0xffffffffu : (1u << p.k) - 1u, mine[w], j) < mine[w];
@@ -735,18 +747,14 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_experts_kernel(const __gri
     }
   }
   const int active = s_active;
-  unsigned* const done = p.sync + kTickets;
-  unsigned* const ready = done + lay.chosen;
-  unsigned* const tile_done = ready + lay.chosen;
-  unsigned* const largest = tile_done + p.tiles;
-  unsigned char* const known = reinterpret_cast<unsigned char*>(mask);  // (masks are in ch.tokens by now) experts seen ready
+  unsigned* const largest = p.sync + kCounters;
 
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
-  for (int e = tid; e < active; e += kMoeThreads) known[e] = 0;
+  const int items1 = active * p.unit_blocks, items2 = active * p.tiles;
   {
-    const GateUp job{p, ch, done, largest, lay.staged ? digits : p.xd, lay.staged ? x_staged : p.x_pitch};
-    run_phase<NT, kGrid, kDepth1>(job, active * p.unit_blocks, p.steps, p.ks[0], &p.sync[0], s_block[0], s_next, acc, ring1, lane, warp);
+    const GateUp job{p, ch, largest, lay.staged ? digits : p.xd, lay.staged ? x_staged : p.x_pitch};
+    run_phase<NT, kGrid, depth1_of(NT)>(job, items1, p.steps, p.ks[0], &p.sync[kBlocks1], &p.sync[kDone1], s_block[0], s_next, acc, ring1, lane, warp);
   }
   auto draw = [&](unsigned* ticket) {
     int v = 0;
@@ -755,20 +763,19 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_experts_kernel(const __gri
   };
   // ---- the rows of inner activations become digits, a warp a row
   if (!p.direct) {
-    for (int row; (row = draw(&p.sync[4])) < lay.rows;) {
-      const int a = ch.row_at[row];
-      if (!wait_counted(&done[a], (unsigned)p.unit_blocks, &gave_up, p.status)) break;
+    for (int row; (row = draw(&p.sync[kRows])) < lay.rows;) {
+      if (!wait_counted(&p.sync[kDone1], (unsigned)items1, &gave_up, p.status)) break;
       make_digits(p, row, __ldcg(largest + row), lane);
       __syncwarp();
-      if (lane == 0) add_release(&ready[a], 1u);
+      if (lane == 0) add_release(&p.sync[kDoneRows], 1u);
     }
   }
   __syncthreads();
-  const Down job{p, ch, done, ready, largest, tile_done, known, &gave_up, own, lay.room, active};
-  run_phase<NT, kGrid, kLater>(job, active * p.tiles, (p.I + 63) >> 6, p.ks[1], &p.sync[2], s_block[1], s_next, acc, ring2, lane, warp);
+  const Down job{p, ch, largest, &p.sync[p.direct ? kDone1 : kDoneRows], (unsigned)(p.direct ? items1 : lay.rows), &s_known, &gave_up, own};
+  run_phase<NT, kGrid, kLater>(job, items2, (p.I + 63) >> 6, p.ks[1], &p.sync[kBlocks2], &p.sync[kDone2], s_block[1], s_next, acc, ring2, lane, warp);
   // ---- the results, a warp a tile of sixteen channels
-  for (int t; (t = draw(&p.sync[5])) < p.tiles;) {
-    if (!wait_counted(&tile_done[t], (unsigned)active, &gave_up, p.status)) break;
+  for (int t; (t = draw(&p.sync[kTiles])) < p.tiles;) {
+    if (!wait_counted(&p.sync[kDone2], (unsigned)items2, &gave_up, p.status)) break;
     job.add_up(t, lane);
   }
 }
@@ -809,7 +816,7 @@ size_t moe_space(const q8_moe_desc& d, char* ws, MoeParams* p) {
   auto take = [&](size_t bytes) { char* q = ws + at; at += up256(bytes); return q; };
   p->logits = reinterpret_cast<double*>(take(T * d.E * sizeof(double)));
   p->x_factor = reinterpret_cast<float*>(take(T * 4));
-  p->sync = reinterpret_cast<unsigned*>(take((kTickets + 3 * rows + (size_t)(d.C + 15) / 16) * 4));
+  p->sync = reinterpret_cast<unsigned*>(take((kCounters + rows) * 4));
   p->xd = reinterpret_cast<signed char*>(take(T * 3 * pitch128(d.C)));
   p->hd = reinterpret_cast<signed char*>(take(rows * 3 * pitch128(d.I)));
   p->part = reinterpret_cast<float*>(take(rows * d.C * 4));
@@ -818,11 +825,11 @@ size_t moe_space(const q8_moe_desc& d, char* ws, MoeParams* p) {
 }
 
 // How many warps share the reduction of an item: the fewest rounds times steps, a round costing about four steps besides.
-int warps_per_item(double items, int steps) {
+int warps_per_item(double items, int steps, int warps) {
   int best = 1;
   double least = 1e30;
   for (int ks = 1; ks <= 4; ks *= 2) {
-    const double cost = ceil(items / (sm_count() * (kMoeWarps / ks))) * ((steps + ks - 1) / ks + 4);
+    const double cost = ceil(items / (sm_count() * (warps / ks))) * ((steps + ks - 1) / ks + 4);
     if (cost < least) { least = cost; best = ks; }
   }
   return best;
@@ -842,7 +849,7 @@ int launch_experts(MoeParams p, cudaStream_t s) {
   }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)sm_count());
-  cfg.blockDim = dim3(kMoeThreads);
+  cfg.blockDim = dim3(32 * warps_of(NT));
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = s;
   cudaLaunchAttribute at[1];
@@ -862,8 +869,9 @@ int launch_experts(const MoeParams& p, cudaStream_t s) {
 }
 
 int launch_route(const MoeParams& p, cudaStream_t s) {
+  const int per = p.T == 1 ? 1 : 4;  // tokens of a block
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(p.T + p.E));
+  cfg.gridDim = dim3((unsigned)(p.T + p.E * ((p.T + per - 1) / per)));
   cfg.blockDim = dim3(256);
   cfg.stream = s;
   cudaLaunchAttribute at[1];
@@ -871,7 +879,7 @@ int launch_route(const MoeParams& p, cudaStream_t s) {
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return check_cuda(cudaLaunchKernelEx(&cfg, moe_route_kernel, p), "moe_route_kernel");
+  return check_cuda(cudaLaunchKernelEx(&cfg, per == 1 ? moe_route_kernel<1> : moe_route_kernel<4>, p), "moe_route_kernel");
 }
 
 }  // namespace
@@ -926,8 +934,9 @@ int q8_moe(const q8_moe_desc* d, const void* x, const float* router, const int8_
     double missed = 1.0;
     for (int t = 0; t < p.T; ++t) missed *= 1.0 - (double)p.k / p.E;
     const double chosen = p.E * (1.0 - missed);
-    p.ks[0] = warps_per_item(chosen * p.unit_blocks, p.steps);
-    p.ks[1] = warps_per_item(chosen * p.tiles, (p.I + 63) / 64);
+    const int warps = warps_of(p.T <= 2 ? 1 : (p.T <= 4 ? 2 : 8));
+    p.ks[0] = warps_per_item(chosen * p.unit_blocks, p.steps, warps);
+    p.ks[1] = warps_per_item(chosen * p.tiles, (p.I + 63) / 64, warps);
     const int run = ((p.I + 63) / 64 + p.ks[1] - 1) / p.ks[1];  // steps of a warp
     p.direct = p.T * run <= kDirectSteps ? 3 * p.T * staged_pitch(run) : 0;
     p.x = static_cast<const char*>(x) + (size_t)t0 * p.ldx * e;
