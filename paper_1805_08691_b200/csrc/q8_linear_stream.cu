@@ -114,20 +114,21 @@ __global__ void __launch_bounds__(kSThreads, 2) linear_stream_kernel(const __gri
     r.left = p.C - from;
   };
   auto issue = [&] {
-    while (ring.flying < kSDepth && r_tile < p.tiles && n > 0) {
-      ring.put(r);
-      r.a += 64 * (kSWarps - 1); r.b += 64 * (kSWarps - 1); r.left -= 64 * (kSWarps - 1);
-      if (++r_step == n) {
-        r_step = 0;
-        r_tile += gridDim.x;
-        if (r_tile < p.tiles) begin(r_tile);
-      }
+    const bool live = r_tile < p.tiles && n > 0;
+    ring.put(r, live);
+    if (!live) return;
+    r.a += 64 * (kSWarps - 1); r.b += 64 * (kSWarps - 1); r.left -= 64 * (kSWarps - 1);
+    if (++r_step == n) {
+      r_step = 0;
+      r_tile += gridDim.x;
+      if (r_tile < p.tiles) begin(r_tile);
     }
   };
   begin(r_tile);
   const signed char* const first_a = r.a;
   const signed char* const first_b = r.b;
-  issue();
+#pragma unroll 1
+  for (int u = 0; u < kSDepth; ++u) issue();
 
   if (p.x_type == Q8_S8) {
     const signed char* x = static_cast<const signed char*>(p.x);
@@ -166,6 +167,7 @@ __global__ void __launch_bounds__(kSThreads, 2) linear_stream_kernel(const __gri
 #pragma unroll 2
     for (int s = 0; s < n; ++s) {
       uint4 a, b;
+      ring.wait();
       ring.get(now, a, b);
       issue();
 #pragma unroll

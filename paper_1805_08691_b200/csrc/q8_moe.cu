@@ -46,8 +46,9 @@ __host__ __device__ constexpr int depth1_of(int nt) { return 80 / warps_of(nt); 
 __host__ __device__ constexpr int depth2_of(int nt, int step_bytes) { return (step_bytes == 1024 ? 128 : 96) / warps_of(nt); }
 constexpr float kDigitMax = 8355711.0f;  // 127 (256^2 + 256 + 1)
 // Tickets: blocks and items of phase one, of phase two, rows to be made digits, tiles to be added up; then how many items of
-// phase one, rows and items of phase two are done.
-enum { kBlocks1, kItems1, kBlocks2, kItems2, kRows, kTiles, kDone1, kDoneRows, kDone2, kCounters };
+// phase one, rows and items of phase two are done.  Each on a line of its own: who waits for one does not slow the others.
+enum { kLine = 32, kBlocks1 = 0, kItems1 = kLine, kBlocks2 = 2 * kLine, kItems2 = 3 * kLine, kRows = 4 * kLine, kTiles = 5 * kLine, kDone1 = 6 * kLine,
+       kDoneRows = 7 * kLine, kDone2 = 8 * kLine, kCounters = 9 * kLine };
 constexpr int kDirectSteps = 32; // tokens times steps up to which the readers of inner activations make their digits themselves
 constexpr unsigned kTimeoutMoe = 32u;
 constexpr unsigned long long kMoeWaitNs = 2000000000ull;
@@ -117,31 +118,22 @@ __device__ __forceinline__ DigitScale digit_scale(unsigned max_bits) {
   d.inverse = __fdiv_rn(kDigitMax, m);
   return d;
 }
-// Digits of v, most significant first.  |code| <= 8355711, so each digit fits eight bits.
-__device__ __forceinline__ void digits_of(float v, const DigitScale& s, int& a, int& b, int& c) {
-  const float q = fminf(fmaxf(__fmul_rn(v, s.inverse), -kDigitMax), kDigitMax);
-  const int code = s.inverse == 0.0f ? 0 : __float2int_rn(q);
-  c = (int)(signed char)code;
-  const int r = (code - c) >> 8;
-  b = (int)(signed char)r;
-  a = (r - b) >> 8;
+// Three digits of v in the bytes 2, 1, 0 of a word: the bytes of code + 128 (256^2 + 256 + 1), each less 128.  The code of the
+// row's largest value may round to one above the most that three digits hold.
+__device__ __forceinline__ unsigned digits_of(float v, const DigitScale& s) {
+  return ((unsigned)__float2int_rn(fminf(__fmul_rn(v, s.inverse), kDigitMax)) + 0x808080u) ^ 0x808080u;
 }
-// Four values as one word of each digit.
+// Four values as one word of each digit, most significant first.
 __device__ __forceinline__ void digits_4(const float4 v, const DigitScale& s, unsigned& a, unsigned& b, unsigned& c) {
-  int d[4][3];
-  digits_of(v.x, s, d[0][0], d[0][1], d[0][2]);
-  digits_of(v.y, s, d[1][0], d[1][1], d[1][2]);
-  digits_of(v.z, s, d[2][0], d[2][1], d[2][2]);
-  digits_of(v.w, s, d[3][0], d[3][1], d[3][2]);
-  unsigned w[3];
-#pragma unroll
-  for (int k = 0; k < 3; ++k)
-    w[k] = (unsigned)(d[0][k] & 255) | (unsigned)(d[1][k] & 255) << 8 | (unsigned)(d[2][k] & 255) << 16 | (unsigned)(d[3][k] & 255) << 24;
-  a = w[0]; b = w[1]; c = w[2];
+  const unsigned d0 = digits_of(v.x, s), d1 = digits_of(v.y, s), d2 = digits_of(v.z, s), d3 = digits_of(v.w, s);
+  const unsigned low01 = __byte_perm(d0, d1, 0x5140), low23 = __byte_perm(d2, d3, 0x5140);
+  a = __byte_perm(__byte_perm(d0, d1, 0x0062), __byte_perm(d2, d3, 0x0062), 0x5410);
+  b = __byte_perm(low01, low23, 0x7632);
+  c = __byte_perm(low01, low23, 0x5410);
 }
-// The sum that three digits' accumulators stand for, rounded once.
+// The sum that three digits' accumulators stand for, rounded three times (a, and either step).
 __device__ __forceinline__ float digits_sum(int a, int b, int c) {
-  return __ll2float_rn(((long long)a << 16) + ((long long)b << 8) + (long long)c);
+  return __fmaf_rn(__fmaf_rn(__int2float_rn(a), 256.0f, __int2float_rn(b)), 256.0f, __int2float_rn(c));
 }
 
 // ------------------------------------------------------------------------------------------ router
@@ -287,6 +279,24 @@ __device__ __noinline__ bool wait_counted(const unsigned* counter, unsigned n, v
     }
   }
 }
+// The same for all warps of a block: one of them reads the counter, the others shared memory (2368 warps that read one line of
+// L2 hold up those that write it).  state: 0 at first, 1 while a warp waits, 2 then.
+__device__ __forceinline__ void wait_block(const unsigned* counter, unsigned n, int* state, int* gave_up, unsigned* status) {
+  volatile int* s = state;
+  int seen = 0;
+  if ((threadIdx.x & 31) == 0) { seen = *s; if (seen == 0) seen = atomicCAS(state, 0, 1); }
+  seen = __shfl_sync(0xffffffffu, seen, 0);
+  if (seen == 0) {
+    wait_counted(counter, n, gave_up, status);
+    __syncwarp();
+    __threadfence_block();
+    *s = 2;
+  } else {
+    while (!__all_sync(0xffffffffu, *s == 2)) __nanosleep(50);  // (the warp that waits stops in time)
+  }
+  __threadfence_block();
+}
+
 
 __device__ __forceinline__ float4 load_h4(const MoeParams& p, int row, int i) {
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -329,7 +339,7 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
     else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
   };
   const bool more = blocks * groups < items;
-  auto draw = [&]() -> int { return more ? blocks * groups + (int)atomicAdd(tickets + 1, 1u) : items; };
+  auto draw = [&]() -> int { return more ? blocks * groups + (int)atomicAdd(tickets + kLine, 1u) : items; };
   int taken = block, taken_at = group;  // the block whose first items this group does, and which of them is next
   int cur = taken < blocks ? taken + blocks * taken_at : items;
   taken_at = groups;
@@ -341,20 +351,19 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
   Ring<kGrid, kDepth> ring;
   ring.init(ring_at, lane);
   unsigned finished = 0;
+  const int slots = max(n, kDepth);  // of an item: with fewer steps than the ring has slots, some stay empty
   for (;;) {
-    Rows r = job.rows(cur, items, s0, n, lane), next = r;
-    int m = cur < items ? n : 0;  // steps of r not copied yet
+    Rows r = job.rows(cur, items, s0, n, lane);
 #pragma unroll 1
-    for (; m > 0 && ring.flying < kDepth; --m) ring.put(r);
+    for (int u = 0; u < kDepth; ++u) ring.put(r, cur < items && u < n);
     meet();
     while (cur < items) {
       const int nxt = s_next[group];
       meet();
       unsigned drawn = (unsigned)items;  // (waited for behind the stream)
       if (gtid == 0 && nxt < items) drawn = (unsigned)draw();
-      const Rows now = r;  // for the alignment of its rows alone
-      if (nxt < items) next = job.rows(nxt, items, s0, n, lane);
-      bool ahead = false;  // r is the next item's
+      const Rows now = r;                // for the alignment of its rows alone
+      Rows next = job.rows(nxt, items, s0, n, lane);
       const int count = job.count(cur);
       const float2 scales = job.scales(cur, g);
       auto go = [&](auto nt) {
@@ -364,46 +373,45 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
 #pragma unroll
         for (int t = 0; t < N; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0;
         job.columns(cur, count, s0, n, lane, z);
-        // digits a batch of steps ahead: from L2 they take as long as a few steps
-        constexpr int A = N <= 2 ? 4 : (N <= 4 ? 2 : 1);
-        uint4 q[A][N];
-        auto fetch = [&](uint4 (&v)[A][N], int s) {
+        // digits two steps ahead: from L2 they take as long as a few steps of the scheduler's other warps.  (Reads behind an
+        // item's last step stay inside the workspace or shared memory and are not used.)
+        constexpr int A = N <= 4 ? 2 : 1;
+        uint4 q[2][A][N];
+        auto fetch = [&](int half) {
 #pragma unroll
           for (int j = 0; j < A; ++j)
 #pragma unroll
-            for (int t = 0; t < N; ++t)
-              if (s + j < n) v[j][t] = *reinterpret_cast<const uint4*>(z[t] + 64 * (s + j));
+            for (int t = 0; t < N; ++t) q[half][j][t] = *reinterpret_cast<const uint4*>(z[t] + 64 * j);
+#pragma unroll
+          for (int t = 0; t < N; ++t) z[t] += 64 * A;
         };
-        if (N <= 4) fetch(q, 0);
-#pragma unroll 1
-        for (int s = 0; s < n; s += A) {
-          uint4 v[A][N];
-          if (N <= 4) fetch(v, s + A);
+        auto step = [&](const uint4 (&v)[N]) {
+          uint4 a, b;
+          ring.get(now, a, b);
+#pragma unroll
+          for (int t = 0; t < N; ++t) {
+            mma_16x8x32(d[t], a.x, b.x, a.y, b.y, v[t].x, v[t].y);
+            mma_16x8x32(d[t], a.z, b.z, a.w, b.w, v[t].z, v[t].w);
+          }
+        };
+        const int ahead = slots - kDepth;  // behind this step, the steps of the next item are copied
+        fetch(0);
+        auto half = [&](int h, int s) {
+          fetch(h ^ 1);
 #pragma unroll
           for (int j = 0; j < A; ++j) {
-            if (s + j >= n) break;
-            uint4 a, b;
-            ring.get(now, a, b);
+            if (s + j >= slots) break;
+            ring.wait();
+            if (s + j < n) step(q[h][j]);
+            if (s + j == ahead) r = next;
+            ring.put(r, s + j < ahead || (nxt < items && s + j - ahead < n));
+          }
+        };
 #pragma unroll 1
-            do {
-              if (m == 0 && !ahead && nxt < items) { r = next; m = n; ahead = true; }
-              if (m == 0) break;
-              ring.put(r);
-              --m;
-            } while (ring.flying < kDepth);
-#pragma unroll
-            for (int t = 0; t < N; ++t) {
-              if (N > 4) q[j][t] = *reinterpret_cast<const uint4*>(z[t] + 64 * (s + j));
-              mma_16x8x32(d[t], a.x, b.x, a.y, b.y, q[j][t].x, q[j][t].y);
-              mma_16x8x32(d[t], a.z, b.z, a.w, b.w, q[j][t].z, q[j][t].w);
-            }
-          }
-          if (N <= 4) {
-#pragma unroll
-            for (int j = 0; j < A; ++j)
-#pragma unroll
-              for (int t = 0; t < N; ++t) q[j][t] = v[j][t];
-          }
+        for (int s = 0; s < slots; s += 2 * A) {
+          half(0, s);
+          if (s + A >= slots) break;
+          half(1, s + A);
         }
         if (gtid == 0) s_next[group] = (int)drawn;
         if (ks > 1) {
@@ -427,6 +435,7 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
           // lanes of even i hold the first two digits of token 2 t + i / 2, their neighbours the third
 #pragma unroll
           for (int t = 0; t < N; ++t) {
+            if (2 * t >= count) break;
             const int third_a = __shfl_xor_sync(0xffffffffu, d[t][0], 1), third_b = __shfl_xor_sync(0xffffffffu, d[t][2], 1);
             const int token = 2 * t + (i >> 1);
             job.finish(cur, token, g, !(i & 1) && token < count, digits_sum(d[t][0], d[t][1], third_a), digits_sum(d[t][2], d[t][3], third_b), scales);
@@ -467,6 +476,7 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
 // Shared memory of a block: lists of rows; partial sums of warps that share items; then the warps' rings and digits, the tokens'
 // in phase one if there is room, a warp's own in phase two.  The logits' keys [T][E] lie over sums and rings until the choice
 // is made.
+constexpr int kOverread = 512;     // bytes behind digits that may be read, and are not used
 constexpr int kMoeSmem = 226 * 1024;
 struct MoeShared {
   int rows, chosen, acc_at, rings_at, digits_at, staged, own_at, room, total;
@@ -478,9 +488,9 @@ struct MoeShared {
     digits_at = rings_at + warps_of(nt) * depth1_of(nt) * step_bytes;
     if (digits_at < acc_at + 8 * T * E) digits_at = acc_at + 8 * T * E;
     const int all = 3 * T * staged_pitch(steps);
-    staged = all <= kMoeSmem - digits_at;
+    staged = all + kOverread <= kMoeSmem - digits_at;
     own_at = rings_at + warps_of(nt) * depth2_of(nt, step_bytes) * step_bytes;
-    room = ((kMoeSmem - own_at) / warps_of(nt)) & ~127;
+    room = ((kMoeSmem - kOverread - own_at) / warps_of(nt)) & ~127;
     total = kMoeSmem;
   }
 };
@@ -522,7 +532,7 @@ struct GateUp {
     if (live && i < p.I) {
       const float f = p.x_factor[ch.row_token[row]];
       const float g = __fmul_rn(__fmul_rn(gate, f), s.x), v = __fmul_rn(__fmul_rn(up, f), s.y);
-      const float h = __fmul_rn(__fdiv_rn(g, __fadd_rn(1.0f, expf(-g))), v);
+      const float h = __fmul_rn(__fdividef(g, __fadd_rn(1.0f, expf(-g))), v);  // (divided within 2 ulp, or 0 for gates below -87)
       p.h[(size_t)row * p.h_pitch + i] = h;
       m = abs_word(h);
     }
@@ -541,7 +551,7 @@ struct Down {
   const unsigned* largest;
   const unsigned* waited;  // a counter and what it has to reach before digits are read
   unsigned reached;
-  int *known, *gave_up;    // (shared memory) whether a warp of this block has seen it
+  int *known, *gave_up;    // (shared memory) see wait_block
   signed char* mine;  // shared memory of this warp for an item's digits
   __device__ __forceinline__ int expert(int item) const { return p.by_tiles(item); }
   __device__ __forceinline__ int count(int item) const { return __popc(ch.tokens[expert(item)]); }
@@ -558,9 +568,7 @@ struct Down {
   template <int NT>
   __device__ __forceinline__ void columns(int item, int count, int s0, int n, int lane, const signed char* (&z)[NT]) const {
     const int a = expert(item), first = ch.first[a], digit = min((lane >> 2) & 3, 2);
-    if (!__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(known)) && wait_counted(waited, reached, gave_up, p.status))
-      *reinterpret_cast<volatile int*>(known) = 1;
-    __threadfence_block();
+    wait_block(waited, reached, known, gave_up, p.status);
     if (!p.direct) {
       const signed char* from = p.hd + (size_t)first * 3 * p.h_pitch + 64 * s0 + 16 * (lane & 3);
 #pragma unroll
@@ -817,8 +825,8 @@ size_t moe_space(const q8_moe_desc& d, char* ws, MoeParams* p) {
   p->logits = reinterpret_cast<double*>(take(T * d.E * sizeof(double)));
   p->x_factor = reinterpret_cast<float*>(take(T * 4));
   p->sync = reinterpret_cast<unsigned*>(take((kCounters + rows) * 4));
-  p->xd = reinterpret_cast<signed char*>(take(T * 3 * pitch128(d.C)));
-  p->hd = reinterpret_cast<signed char*>(take(rows * 3 * pitch128(d.I)));
+  p->xd = reinterpret_cast<signed char*>(take(T * 3 * pitch128(d.C) + kOverread));
+  p->hd = reinterpret_cast<signed char*>(take(rows * 3 * pitch128(d.I) + kOverread));
   p->part = reinterpret_cast<float*>(take(rows * d.C * 4));
   p->h = reinterpret_cast<float*>(take(rows * pitch128(d.I) * 4));
   return at;

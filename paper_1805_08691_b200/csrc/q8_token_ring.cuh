@@ -29,12 +29,12 @@ struct Ring {
   static constexpr int kStep = kGrid == 1 ? 1280 : 1024, kHalf = kStep / 2, kBytes = kDepth * kStep;
   const unsigned char* at;  // this lane's bytes of slot 0
   uint32_t to;
-  int in, out;              // bytes from there to the slots of the next step copied and used
-  int flying;               // steps between them
+  int slot;                 // bytes to the slot of the next step, in use and then free: the ring is always full, if only of
+                            // groups without copies, so that a group of copies is a slot
   __device__ __forceinline__ void init(const unsigned char* ring, int lane) {
     at = ring + (kGrid == 1 ? 4 : 16) * lane;
     to = (uint32_t)__cvta_generic_to_shared(at);
-    in = out = flying = 0;
+    slot = 0;
   }
   template <int kBytes>
   static __device__ __forceinline__ void copy(uint32_t dst, const void* src, bool live) {
@@ -65,24 +65,23 @@ struct Ring {
       return make_uint4(__funnelshift_r(u[0], u[1], m), __funnelshift_r(u[1], u[2], m), __funnelshift_r(u[2], u[3], m), __funnelshift_r(u[3], u[4], m));
     }
   }
-  __device__ __forceinline__ void put(Rows& r) {
-    copy_row(to + in, r.a, r.left);
-    copy_row(to + in + kHalf, r.b, r.left);
-    r.a += 64;
-    r.b += 64;
-    r.left -= 64;
+  // The step at r into the present slot (live: there is one), and on to the next slot.
+  __device__ __forceinline__ void put(Rows& r, bool live) {
+    if (live) {
+      copy_row(to + slot, r.a, r.left);
+      copy_row(to + slot + kHalf, r.b, r.left);
+      r.a += 64;
+      r.b += 64;
+      r.left -= 64;
+    }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    in = in == (kDepth - 1) * kStep ? 0 : in + kStep;
-    ++flying;
+    slot = slot == (kDepth - 1) * kStep ? 0 : slot + kStep;
   }
+  // The step in the present slot, the oldest; a and b have the alignment of its rows.  put() follows.
+  __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory"); }
   __device__ __forceinline__ void get(const Rows& r, uint4& a, uint4& b) {
-    // a group for each step: with a full ring the oldest is done when all but the others are
-    if (flying == kDepth) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
-    else asm volatile("cp.async.wait_group 0;" ::: "memory");
-    --flying;
-    a = read_row(at + out, r.a);
-    b = read_row(at + out + kHalf, r.b);
-    out = out == (kDepth - 1) * kStep ? 0 : out + kStep;
+    a = read_row(at + slot, r.a);
+    b = read_row(at + slot + kHalf, r.b);
   }
 };
 
