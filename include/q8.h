@@ -454,7 +454,7 @@ int q8_linear(const q8_linear_desc* d, const void* x, const float* x_scale, cons
  *   g = (x . w_gate_up[e][i]) * s_gate_up[e][i],  u = (x . w_gate_up[e][I + i]) * s_gate_up[e][I + i],  i < I
  *   h[i] = g / (1 + exp(-g)) * u
  *   y[t][c] = sum over the chosen e of p * ((h . w_down[e][c]) * s_down[e][c])
- * Activations and h are not rounded to 8 bits: they keep at least 22 bits below the largest of their row, and results are
+ * Activations and h are not rounded to 8 bits: they keep 24 bits or more, of the largest of their row or of their own, and results are
  * those of 32-bit arithmetic.  The same inputs give the same bits whatever the other tokens of the call are. */
 typedef struct q8_moe_desc {
   int64_t ldx, ldy;         /* elements from one token to the next; 0: C */

@@ -24,8 +24,7 @@ int validate_linear(const q8_linear_desc* d, LinearArgs* a) {
   return Q8_OK;
 }
 
-// Rows of bytes onto the 16-byte grid, zeros behind their ends: thread = 16 bytes, from aligned words each of which holds a
-// byte of the row.
+// Rows of bytes onto the 16-byte grid, zeros behind their ends: thread = 16 bytes.
 __global__ void __launch_bounds__(256) regrid_kernel(const signed char* __restrict__ in, long long rows, int C, long long ld, signed char* __restrict__ out,
                                                      int pitch) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -34,20 +33,8 @@ __global__ void __launch_bounds__(256) regrid_kernel(const signed char* __restri
   const long long n = rows * chunks;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
     const long long r = i / chunks;
-    const int c = (int)(i - r * chunks) * 16, left = C - c;
-    const unsigned long long at = (unsigned long long)(in + r * ld + c);
-    const unsigned* w = reinterpret_cast<const unsigned*>(at & ~3ull);
-    const int m = (int)(at & 3ull);
-    unsigned u[5], v[4];
-#pragma unroll
-    for (int k = 0; k < 5; ++k) u[k] = 4 * k - m < left && (k < 4 || m > 0) ? __ldg(w + k) : 0u;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      v[k] = __funnelshift_r(u[k], u[k + 1], 8 * m);
-      const int valid = left - 4 * k;
-      if (valid < 4) v[k] &= valid <= 0 ? 0u : (1u << (8 * valid)) - 1u;
-    }
-    *reinterpret_cast<uint4*>(out + r * pitch + c) = make_uint4(v[0], v[1], v[2], v[3]);
+    const int c = (int)(i - r * chunks) * 16;
+    *reinterpret_cast<uint4*>(out + r * pitch + c) = load_16<false>(in + r * ld, c, C);
   }
 }
 int regrid(const int8_t* in, long long rows, int C, long long ld, int8_t* out, int pitch, cudaStream_t s) {

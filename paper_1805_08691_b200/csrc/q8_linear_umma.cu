@@ -35,7 +35,8 @@ struct LinearParams {
   const float* bias;
   void* y;
   long long ldy;
-  int y_vec;                  // rows of y on the 16-byte grid
+  int y_vec;                  // rows of y on the 16-byte grid; else warps exchange 32 x 32 results and store along rows
+  unsigned off_turn;          // where they do, in shared memory
   unsigned* status;
 };
 
@@ -57,8 +58,8 @@ __device__ __forceinline__ void tile_of(const LinearParams& p, int tile, int* mt
 }
 
 template <typename T>
-__device__ __forceinline__ void store_16(T* y, const float (&v)[16], int valid, bool vec) {
-  if (vec && valid >= 16) {
+__device__ __forceinline__ void store_16(T* y, const float (&v)[16], int valid) {
+  if (valid >= 16) {
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) reinterpret_cast<float4*>(y)[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
@@ -178,6 +179,7 @@ __global__ void __launch_bounds__(kLThreads, 1) __cluster_dims__(2, 1, 1)
   } else {
     const int e = warp - 2, quad = warp & 3, group = e >> 2, tid = (int)threadIdx.x - 64;
     const int chunks = p.bn >> 4, per = (chunks + 1) >> 1, c0 = group * per, c1 = min(chunks, c0 + per);
+    float* const turn = reinterpret_cast<float*>(smem_raw + (base - raw) + p.off_turn) + e * (32 * 33);
     uint32_t ab = 0, par = 0;
     bool ok = true;
     for (int tile = first; tile < tiles; tile += step) {
@@ -215,7 +217,24 @@ __global__ void __launch_bounds__(kLThreads, 1) __cluster_dims__(2, 1, 1)
 #pragma unroll
           for (int j = 0; j < 16; ++j) f[j] = __fadd_rn(f[j], s_bias[ab][c * 16 + j]);
         }
-        if (live) store_16(row + c * 16, f, p.K - n0 - c * 16, p.y_vec);
+        if (p.y_vec) {
+          if (live) store_16(row + c * 16, f, p.K - n0 - c * 16);
+        } else {
+          // a lane has sixteen columns of its row: two chunks make a square, which leaves row by row
+          const int c_in = (c - c0) & 1;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) turn[lane * 33 + c_in * 16 + j] = f[j];
+          if (c_in || c + 1 == c1) {
+            __syncwarp();
+            const int col = (c - c_in) * 16 + lane, rows = (int)min(32ll, (long long)p.M - (m - lane));
+            const bool there = lane < (c_in ? 32 : 16) && n0 + col < p.K;
+            T* out = static_cast<T*>(p.y) + (m - lane) * p.ldy + n0 + col;
+#pragma unroll 8
+            for (int q = 0; q < rows; ++q)
+              if (there) out[(long long)q * p.ldy] = from_f32<T>(turn[q * 33 + lane]);
+            __syncwarp();
+          }
+        }
       };
       int va[16], vb[16];
       if (c0 < c1) tmem_ld_16(t + c0 * 16, va);
@@ -314,13 +333,14 @@ int launch_linear_umma(const LinearArgs& a) {
   p.kb = p.bn <= 128 ? blocks_per_load(a.C) : 1;  // (wide tiles are long enough: 46.6 us with one block, 48.2 with two)
   p.off_w = (unsigned)p.kb * kLABytes;
   p.stage_bytes = p.off_w + (unsigned)(p.kb * (p.bn / 2)) * kLBK;
-  p.stages = (int)((kSmemLimit - 8192 - 1024) / p.stage_bytes);
+  p.y_vec = aligned16(a.y) && a.ldy * (long long)type_bytes(a.y_type) % 16 == 0;
+  const unsigned turn_bytes = p.y_vec ? 0u : kLEpiWarps * 32u * 33u * 4u;
+  p.stages = (int)((kSmemLimit - 8192 - 1024 - turn_bytes) / p.stage_bytes);
   if (p.stages > kLMaxStages) p.stages = kLMaxStages;
   p.idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((unsigned)(p.bn >> 3) << 17) | ((256u >> 4) << 24);
   p.desc_hi = (unsigned)((8 * kLBK) >> 4) | (1u << 14) | (2u << 29);
   p.x_scale = a.x_scale; p.w_scale = a.w_scale; p.bias = a.bias;
   p.y = a.y; p.ldy = a.ldy;
-  p.y_vec = aligned16(a.y) && a.ldy * (long long)type_bytes(a.y_type) % 16 == 0;
   p.status = status_word_device_ptr();
   if (!p.status) return fail(Q8_ERR_CUDA, "linear_umma: status word not available");
   CUtensorMap tmX, tmW;
@@ -329,7 +349,8 @@ int launch_linear_umma(const LinearArgs& a) {
   if (rc != Q8_OK) return rc;
   const long long tiles = (long long)p.m_tiles * p.n_tiles, pairs = sm_count() / 2;
   const int grid = 2 * (int)(tiles < pairs ? tiles : pairs);
-  const size_t dyn = 1024 + (size_t)p.stages * p.stage_bytes;
+  p.off_turn = (unsigned)p.stages * p.stage_bytes;
+  const size_t dyn = 1024 + (size_t)p.off_turn + turn_bytes;
   if (a.y_type == Q8_F32) return launch_pairs<float>(tmX, tmW, p, grid, dyn, a.stream);
   if (a.y_type == Q8_F16) return launch_pairs<__half>(tmX, tmW, p, grid, dyn, a.stream);
   return launch_pairs<__nv_bfloat16>(tmX, tmW, p, grid, dyn, a.stream);

@@ -8,10 +8,11 @@
 //                       of eight inner units (their eight gate and eight up rows are the sixteen rows of an instruction),
 //                       then of sixteen output channels of an expert.
 //
-// A value of a token is held as a 24-bit integer relative to the row's largest, in three digits to the base 256 of -128 ..
-// 127: the digits are columns of an 8-bit product like tokens, four to a token with one left idle, so that the eight columns
-// of mma.sync.m16n8k32 take two tokens.  Weights enter the tensor cores as the bytes they are, no conversion; all sums are
-// exact integers, so neither the split of a reduction over warps nor the order of their additions changes a bit.
+// A value of a token is held as a 32-bit integer relative to the row's largest, in four digits to the base 256 of -128 ..
+// 127: the digits are columns of an 8-bit product like tokens, so that the eight columns of mma.sync.m16n8k32 take two tokens.
+// Weights enter the tensor cores as the bytes they are, no conversion; all sums are exact integers, so neither the split of
+// a reduction over warps nor the order of their additions changes a bit.  (With three digits the fourth column would be
+// idle, and rows with a few large values lost a few bits of the small ones: 1.0e-6 of the result against 2.4e-7 in fp32.)
 //
 // The order of the products inside an instruction is free as long as both operands share it: a lane's 16 contiguous bytes of
 // a weight row are its operands of two instructions as they come.  They reach the lane through a ring of its warp in shared
@@ -39,12 +40,12 @@ constexpr int kMaxTopK = 32;      // a lane each
 constexpr int kMaxExperts = 1024; // a bit of a lane's word each
 // Warps of a block, by the eights of columns of its kernel: with many columns a warp needs more than 128 registers.
 __host__ __device__ constexpr int warps_of(int nt) { return nt > 2 ? 8 : 16; }
-// Steps of 16 x 64 bytes in a warp's ring: 80 KiB of weights on their way to an SM in phase one, 128 KiB in phase two, whose
-// items are shorter and have more to wait for.  (kGrid 1: a step takes 1280 bytes.  The depths are chosen so that `room` in
-// MoeShared holds a step of every token's digits, 192 T bytes, within all limits.)
-__host__ __device__ constexpr int depth1_of(int nt) { return 80 / warps_of(nt); }
+// Steps of 16 x 64 bytes in a warp's ring: 80 KiB of weights on their way to an SM in phase one (64 with many tokens, whose
+// digits take the room), 128 KiB in phase two, whose items are shorter and have more to wait for.  (kGrid 1: a step takes 1280
+// bytes.)
+__host__ __device__ constexpr int depth1_of(int nt) { return (nt > 2 ? 64 : 80) / warps_of(nt); }
 __host__ __device__ constexpr int depth2_of(int nt, int step_bytes) { return (step_bytes == 1024 ? 128 : 96) / warps_of(nt); }
-constexpr float kDigitMax = 8355711.0f;  // 127 (256^2 + 256 + 1)
+constexpr float kDigitMax = 2139062016.0f;  // the largest fp32 number below 127 (256^3 + 256^2 + 256 + 1)
 // Tickets: blocks and items of phase one, of phase two, rows to be made digits, tiles to be added up; then how many items of
 // phase one, rows and items of phase two are done.  Each on a line of its own: who waits for one does not slow the others.
 enum { kLine = 32, kBlocks1 = 0, kItems1 = kLine, kBlocks2 = 2 * kLine, kItems2 = 3 * kLine, kRows = 4 * kLine, kTiles = 5 * kLine, kDone1 = 6 * kLine,
@@ -76,8 +77,8 @@ struct MoeParams {
   float* x_factor;       // [T]
   unsigned* sync;        // tickets and counters (kBlocks1 ..), then the largest magnitude of each row
   float* part;           // weighted results of the experts [T k][C]
-  signed char* xd;       // digits of the tokens [T][3][x_pitch]
-  signed char* hd;       // digits of the inner activations [T k][3][h_pitch]
+  signed char* xd;       // digits of the tokens [T][4][x_pitch]
+  signed char* hd;       // digits of the inner activations [T k][4][h_pitch]
   float* h;              // inner activations [T k][h_pitch]
   int x_pitch, h_pitch;  // multiples of 128
   int unit_blocks, tiles, steps;  // items of an expert in phase one; items of phase two; steps of an item of phase one
@@ -106,35 +107,36 @@ __device__ __forceinline__ float4 load_x4(const MoeParams& p, int t, int c) {
   return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
 }
 
-// Factor of a row's digits and its reciprocal.  Maxima below 2^-104 take a power of two, whose reciprocal is finite; a row
-// with a NaN or an infinity has factor NaN and digits zero.
+// Factor of a row's digits and its reciprocal.  Maxima below 2^-95 take a power of two, whose reciprocal is finite; a row
+// with a NaN or an infinity has factor NaN, and its digits do not matter.
 struct DigitScale { float factor, inverse; };
 __device__ __forceinline__ DigitScale digit_scale(unsigned max_bits) {
   DigitScale d;
   if (max_bits >= 0x7f800000u) { d.factor = __uint_as_float(0x7fc00000u); d.inverse = 0.0f; return d; }
   const float m = __uint_as_float(max_bits);
-  if (m < 0x1p-104f) { d.factor = 0x1p-126f; d.inverse = 0x1p126f; return d; }
+  if (m < 0x1p-95f) { d.factor = 0x1p-126f; d.inverse = 0x1p126f; return d; }
   d.factor = __fdiv_rn(m, kDigitMax);
   d.inverse = __fdiv_rn(kDigitMax, m);
   return d;
 }
-// Three digits of v in the bytes 2, 1, 0 of a word: the bytes of code + 128 (256^2 + 256 + 1), each less 128.  The code of the
-// row's largest value may round to one above the most that three digits hold.
+// The digits of v, the most significant in the highest byte of a word: the bytes of code + 128 (256^3 + 256^2 + 256 + 1), each
+// less 128.  (The product with the reciprocal may round up to one fp32 step above the most that the digits hold.)
 __device__ __forceinline__ unsigned digits_of(float v, const DigitScale& s) {
-  return ((unsigned)__float2int_rn(fminf(__fmul_rn(v, s.inverse), kDigitMax)) + 0x808080u) ^ 0x808080u;
+  return ((unsigned)__float2int_rn(fminf(__fmul_rn(v, s.inverse), kDigitMax)) + 0x80808080u) ^ 0x80808080u;
 }
 // Four values as one word of each digit, most significant first.
-__device__ __forceinline__ void digits_4(const float4 v, const DigitScale& s, unsigned& a, unsigned& b, unsigned& c) {
+__device__ __forceinline__ void digits_4(const float4 v, const DigitScale& s, unsigned (&d)[4]) {
   const unsigned d0 = digits_of(v.x, s), d1 = digits_of(v.y, s), d2 = digits_of(v.z, s), d3 = digits_of(v.w, s);
   const unsigned low01 = __byte_perm(d0, d1, 0x5140), low23 = __byte_perm(d2, d3, 0x5140);
-  a = __byte_perm(__byte_perm(d0, d1, 0x0062), __byte_perm(d2, d3, 0x0062), 0x5410);
-  b = __byte_perm(low01, low23, 0x7632);
-  c = __byte_perm(low01, low23, 0x5410);
+  const unsigned high01 = __byte_perm(d0, d1, 0x7362), high23 = __byte_perm(d2, d3, 0x7362);
+  d[0] = __byte_perm(high01, high23, 0x7632);
+  d[1] = __byte_perm(high01, high23, 0x5410);
+  d[2] = __byte_perm(low01, low23, 0x7632);
+  d[3] = __byte_perm(low01, low23, 0x5410);
 }
-// The sum that three digits' accumulators stand for, rounded three times (a, and either step).
-__device__ __forceinline__ float digits_sum(int a, int b, int c) {
-  return __fmaf_rn(__fmaf_rn(__int2float_rn(a), 256.0f, __int2float_rn(b)), 256.0f, __int2float_rn(c));
-}
+// The sum that two digits' accumulators stand for, rounded once at the most (the sum of four: the first two times 65536 and
+// the other two).
+__device__ __forceinline__ float digits_sum(int high, int low) { return __fmaf_rn(__int2float_rn(high), 256.0f, __int2float_rn(low)); }
 
 // ------------------------------------------------------------------------------------------ router
 template <int kTok>
@@ -162,7 +164,7 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
     for (int i = 0; i < 8; ++i) m = max(m, part[i]);
     const DigitScale s = digit_scale(m);
     if (threadIdx.x == 0) p.x_factor[t] = s.factor;
-    signed char* out = p.xd + (size_t)t * 3 * p.x_pitch;
+    signed char* out = p.xd + (size_t)t * 4 * p.x_pitch;
     for (int c = 4 * threadIdx.x; c < p.x_pitch; c += 1024) {
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (p.x_vec) {
@@ -173,11 +175,10 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
         if (c + 2 < p.C) v.z = load_x(p, t, c + 2);
         if (c + 3 < p.C) v.w = load_x(p, t, c + 3);
       }
-      unsigned a, b, d;
-      digits_4(v, s, a, b, d);
-      *reinterpret_cast<unsigned*>(out + c) = a;
-      *reinterpret_cast<unsigned*>(out + p.x_pitch + c) = b;
-      *reinterpret_cast<unsigned*>(out + 2 * (size_t)p.x_pitch + c) = d;
+      unsigned d[4];
+      digits_4(v, s, d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *reinterpret_cast<unsigned*>(out + j * (size_t)p.x_pitch + c) = d[j];
     }
     return;
   }
@@ -309,14 +310,13 @@ __device__ __forceinline__ float4 load_h4(const MoeParams& p, int row, int i) {
 // The digits of one row of inner activations, by a warp; zero behind the row's end.
 __device__ __forceinline__ void make_digits(const MoeParams& p, int row, unsigned largest, int lane) {
   const DigitScale s = digit_scale(largest);
-  signed char* out = p.hd + (size_t)row * 3 * p.h_pitch;
+  signed char* out = p.hd + (size_t)row * 4 * p.h_pitch;
 #pragma unroll 8
   for (int i = 4 * lane; i < p.h_pitch; i += 128) {
-    unsigned a, b, c;
-    digits_4(load_h4(p, row, i), s, a, b, c);
-    *reinterpret_cast<unsigned*>(out + i) = a;
-    *reinterpret_cast<unsigned*>(out + p.h_pitch + i) = b;
-    *reinterpret_cast<unsigned*>(out + 2 * (size_t)p.h_pitch + i) = c;
+    unsigned d[4];
+    digits_4(load_h4(p, row, i), s, d);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<unsigned*>(out + j * (size_t)p.h_pitch + i) = d[j];
   }
 }
 
@@ -432,13 +432,15 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
           __syncwarp();
         }
         if (part == 0) {
-          // lanes of even i hold the first two digits of token 2 t + i / 2, their neighbours the third
+          // lanes of even i hold the first two digits of token 2 t + i / 2, their neighbours the other two
 #pragma unroll
           for (int t = 0; t < N; ++t) {
             if (2 * t >= count) break;
-            const int third_a = __shfl_xor_sync(0xffffffffu, d[t][0], 1), third_b = __shfl_xor_sync(0xffffffffu, d[t][2], 1);
+            float a = digits_sum(d[t][0], d[t][1]), b = digits_sum(d[t][2], d[t][3]);
+            a = __fmaf_rn(a, 65536.0f, __shfl_xor_sync(0xffffffffu, a, 1));
+            b = __fmaf_rn(b, 65536.0f, __shfl_xor_sync(0xffffffffu, b, 1));
             const int token = 2 * t + (i >> 1);
-            job.finish(cur, token, g, !(i & 1) && token < count, digits_sum(d[t][0], d[t][1], third_a), digits_sum(d[t][2], d[t][3], third_b), scales);
+            job.finish(cur, token, g, !(i & 1) && token < count, a, b, scales);
           }
         }
       };
@@ -487,7 +489,7 @@ struct MoeShared {
     rings_at = acc_at + warps_of(nt) / 2 * 512 * nt;
     digits_at = rings_at + warps_of(nt) * depth1_of(nt) * step_bytes;
     if (digits_at < acc_at + 8 * T * E) digits_at = acc_at + 8 * T * E;
-    const int all = 3 * T * staged_pitch(steps);
+    const int all = 4 * T * staged_pitch(steps);
     staged = all + kOverread <= kMoeSmem - digits_at;
     own_at = rings_at + warps_of(nt) * depth2_of(nt, step_bytes) * step_bytes;
     room = ((kMoeSmem - kOverread - own_at) / warps_of(nt)) & ~127;
@@ -516,10 +518,10 @@ struct GateUp {
   }
   template <int NT>
   __device__ __forceinline__ void columns(int item, int count, int s0, int n, int lane, const signed char* (&z)[NT]) const {
-    const int first = ch.first[expert(item)], digit = min((lane >> 2) & 3, 2);
+    const int first = ch.first[expert(item)], digit = (lane >> 2) & 3;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
-      z[t] = digits + (ch.row_token[first + min(2 * t + (lane >> 4), count - 1)] * 3 + digit) * pitch + 64 * s0 + 16 * (lane & 3);
+      z[t] = digits + (ch.row_token[first + min(2 * t + (lane >> 4), count - 1)] * 4 + digit) * pitch + 64 * s0 + 16 * (lane & 3);
   }
   __device__ __forceinline__ float2 scales(int item, int u) const {
     const int a = expert(item), i = min((item - a * p.unit_blocks) * 8 + u, p.I - 1);
@@ -567,12 +569,12 @@ struct Down {
   }
   template <int NT>
   __device__ __forceinline__ void columns(int item, int count, int s0, int n, int lane, const signed char* (&z)[NT]) const {
-    const int a = expert(item), first = ch.first[a], digit = min((lane >> 2) & 3, 2);
+    const int a = expert(item), first = ch.first[a], digit = (lane >> 2) & 3;
     wait_block(waited, reached, known, gave_up, p.status);
     if (!p.direct) {
-      const signed char* from = p.hd + (size_t)first * 3 * p.h_pitch + 64 * s0 + 16 * (lane & 3);
+      const signed char* from = p.hd + (size_t)first * 4 * p.h_pitch + 64 * s0 + 16 * (lane & 3);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) z[t] = from + (size_t)(min(2 * t + (lane >> 4), count - 1) * 3 + digit) * p.h_pitch;
+      for (int t = 0; t < NT; ++t) z[t] = from + (size_t)(min(2 * t + (lane >> 4), count - 1) * 4 + digit) * p.h_pitch;
       return;
     }
     // digits made here, in the warp's own shared memory
@@ -582,17 +584,15 @@ struct Down {
       const DigitScale scale = digit_scale(__ldcg(largest + first + r));
 #pragma unroll 8
       for (int c = 4 * lane; c < len; c += 128) {
-        unsigned d0, d1, d2;
-        digits_4(load_h4(p, first + r, 64 * s0 + c), scale, d0, d1, d2);
-        signed char* to = mine + 3 * r * pitch + c;
-        *reinterpret_cast<unsigned*>(to) = d0;
-        *reinterpret_cast<unsigned*>(to + pitch) = d1;
-        *reinterpret_cast<unsigned*>(to + 2 * pitch) = d2;
+        unsigned d[4];
+        digits_4(load_h4(p, first + r, 64 * s0 + c), scale, d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<unsigned*>(mine + (4 * r + j) * pitch + c) = d[j];
       }
     }
     __syncwarp();
 #pragma unroll
-    for (int t = 0; t < NT; ++t) z[t] = mine + (min(2 * t + (lane >> 4), count - 1) * 3 + digit) * pitch + 16 * (lane & 3);
+    for (int t = 0; t < NT; ++t) z[t] = mine + (min(2 * t + (lane >> 4), count - 1) * 4 + digit) * pitch + 16 * (lane & 3);
   }
   __device__ __forceinline__ float2 scales(int item, int u) const {
     const int a = expert(item), c = 16 * (item - a * p.tiles) + u;
@@ -654,7 +654,7 @@ __global__ void __launch_bounds__(32 * warps_of(NT), 1) moe_experts_kernel(const
   signed char* const own = reinterpret_cast<signed char*>(smem + lay.own_at) + warp * lay.room;
   const int x_staged = staged_pitch(p.steps);
   if (lay.staged) {  // the tokens' digits, on their way during the choice
-    for (int r = warp; r < 3 * p.T; r += kMoeWarps)
+    for (int r = warp; r < 4 * p.T; r += kMoeWarps)
       for (int c = 16 * lane; c < 64 * p.steps; c += 512) copy_async_16(digits + r * x_staged + c, p.xd + (size_t)r * p.x_pitch + c);
   }
   if (tid < 2) s_block[tid] = (int)atomicAdd(&p.sync[tid ? kBlocks2 : kBlocks1], 1u);  // this block's number in either phase
@@ -825,8 +825,8 @@ size_t moe_space(const q8_moe_desc& d, char* ws, MoeParams* p) {
   p->logits = reinterpret_cast<double*>(take(T * d.E * sizeof(double)));
   p->x_factor = reinterpret_cast<float*>(take(T * 4));
   p->sync = reinterpret_cast<unsigned*>(take((kCounters + rows) * 4));
-  p->xd = reinterpret_cast<signed char*>(take(T * 3 * pitch128(d.C) + kOverread));
-  p->hd = reinterpret_cast<signed char*>(take(rows * 3 * pitch128(d.I) + kOverread));
+  p->xd = reinterpret_cast<signed char*>(take(T * 4 * pitch128(d.C) + kOverread));
+  p->hd = reinterpret_cast<signed char*>(take(rows * 4 * pitch128(d.I) + kOverread));
   p->part = reinterpret_cast<float*>(take(rows * d.C * 4));
   p->h = reinterpret_cast<float*>(take(rows * pitch128(d.I) * 4));
   return at;
@@ -946,7 +946,7 @@ int q8_moe(const q8_moe_desc* d, const void* x, const float* router, const int8_
     p.ks[0] = warps_per_item(chosen * p.unit_blocks, p.steps, warps);
     p.ks[1] = warps_per_item(chosen * p.tiles, (p.I + 63) / 64, warps);
     const int run = ((p.I + 63) / 64 + p.ks[1] - 1) / p.ks[1];  // steps of a warp
-    p.direct = p.T * run <= kDirectSteps ? 3 * p.T * staged_pitch(run) : 0;
+    p.direct = p.T * run <= kDirectSteps ? 4 * p.T * staged_pitch(run) : 0;
     p.x = static_cast<const char*>(x) + (size_t)t0 * p.ldx * e;
     p.y = static_cast<char*>(y) + (size_t)t0 * p.ldy * e;
     p.ids = ids ? ids + (size_t)t0 * p.k : nullptr;

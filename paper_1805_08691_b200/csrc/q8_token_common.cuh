@@ -142,16 +142,25 @@ __device__ __forceinline__ unsigned max_two(unsigned m, unsigned w) {
   return d;
 }
 
-// Bytes pos .. pos + 15 of a row of `len` bytes, zero from len on; no byte outside the row is read.  kAligned: the row
-// starts on the 16-byte grid and so does pos.
+// Bytes pos .. pos + 15 of a row of `len` bytes, zero from len on.  kAligned: the row starts on the 16-byte grid and so does
+// pos.  Otherwise from aligned words, each of which holds a byte of the row.
 template <bool kAligned>
 __device__ __forceinline__ uint4 load_16(const signed char* row, int pos, int len) {
   if (kAligned && pos + 16 <= len) return __ldg(reinterpret_cast<const uint4*>(row + pos));
-  unsigned int w[4] = {0u, 0u, 0u, 0u};
+  const int left = len - pos;
+  const unsigned long long at = (unsigned long long)(row + pos);
+  const unsigned* w = reinterpret_cast<const unsigned*>(at & ~3ull);
+  const int m = (int)(at & 3ull);
+  unsigned u[5], v[4];
 #pragma unroll
-  for (int j = 0; j < 16; ++j)
-    if (pos + j < len) w[j >> 2] |= (unsigned int)(unsigned char)row[pos + j] << (8 * (j & 3));
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  for (int k = 0; k < 5; ++k) u[k] = 4 * k - m < left && (k < 4 || m > 0) ? __ldg(w + k) : 0u;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[k] = __funnelshift_r(u[k], u[k + 1], 8 * m);
+    const int valid = left - 4 * k;
+    if (valid < 4) v[k] &= valid <= 0 ? 0u : (1u << (8 * valid)) - 1u;
+  }
+  return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // D (16 x 8, int32) += A (16 x 32) B (32 x 8), 8-bit integers.  Lane 4g + i holds bytes 4i..4i+3 and 16+4i.. of the rows g and
