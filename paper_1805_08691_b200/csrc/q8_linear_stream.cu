@@ -2,14 +2,15 @@
 //
 //   D[16 output channels, 8 NT tokens] (int32, registers) = W[16, C] (rings in shared memory) x Z[8 NT, C]^T (shared memory)
 //
-// A block holds the codes of all tokens in shared memory and walks over tiles of 16 output channels; its eight warps share
+// A block holds the codes of all tokens in shared memory and walks over tiles of 16 output channels; its sixteen warps share
 // the reduction, and their rings of weights run on from tile to tile.  Floating-point activations of a few tokens become codes
 // while they are staged: every block finds the factors itself, which costs less than a launch before it.  What the block
 // will read first is on its way into L2 while the kernel before it drains (a hint, which reads nothing: weights may be
 // that kernel's results).
 //
-// 4096 -> 4096, one token: 4.1 us from codes (4.1 TB/s, the weights partly in L2), 5.2 us from bf16; 4096 -> 11008: 11.2 us
-// (4.0 TB/s).  The form before it, which loaded weights step by step into registers, took 9.6 us for the first.
+// 4096 -> 4096, one token: 4.6 us from codes (3.7 TB/s, weights partly in L2), 5.2 us from bf16; 4096 -> 11008: 9.8 us (4.6
+// TB/s), 8192 -> 8192: 15.3 us (4.4 TB/s): the tiles' ends, where the warps meet, cost a quarter.  The form before it, which
+// loaded weights step by step into registers, took 9.6 us for the first.
 #include <atomic>
 
 #include "q8_linear.h"
@@ -18,9 +19,10 @@
 namespace q8 {
 namespace {
 
-constexpr int kSWarps = 8, kSThreads = 32 * kSWarps;
-constexpr int kSDepth = 6;              // steps of a warp's ring: 48 KiB a block
+constexpr int kSWarps = 16, kSThreads = 32 * kSWarps;
+constexpr int kSDepth = 4;              // steps of a warp's ring: 64 KiB a block (96 KiB: one token 5.5 us instead of 5.2)
 constexpr int kSSmem = 224 * 1024;
+constexpr int kSLeast = 115 * 1024;     // a block an SM: with four, those of a short launch do not reach all SMs (7.9 us)
 
 struct StreamParams {
   int M, C, K, steps, tiles, pitch, x_vec;
@@ -84,7 +86,7 @@ __device__ __forceinline__ void stage_tokens(const StreamParams& p, signed char*
 }
 
 template <int NT, int kGrid>
-__global__ void __launch_bounds__(kSThreads, 2) linear_stream_kernel(const __grid_constant__ StreamParams p) {
+__global__ void __launch_bounds__(kSThreads, 1) linear_stream_kernel(const __grid_constant__ StreamParams p) {
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ TokenFactor s_fac[8 * NT];
   __shared__ unsigned s_max[8 * NT];
@@ -94,14 +96,14 @@ __global__ void __launch_bounds__(kSThreads, 2) linear_stream_kernel(const __gri
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   {
     // the first steps of every warp
-    const int row = blockIdx.x * 16 + (tid >> 4);
+    const int row = blockIdx.x * 16 + (tid >> 4 & 15);
     const long long at = (long long)min(row, p.K - 1) * p.ldw + (tid & 15) * 128;
     if ((tid & 15) * 128 < p.C) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.w + at));
     if ((tid & 15) * 128 + 2048 < p.C) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.w + at + 2048));
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  // a warp takes every eighth step of a tile
+  // a warp takes every sixteenth step of a tile
   const int n = (p.steps - warp + kSWarps - 1) / kSWarps;  // steps of a tile that are this warp's
   Ring<kGrid, kSDepth> ring;
   ring.init(smem + warp * Ring<kGrid, kSDepth>::kBytes, lane);
@@ -172,7 +174,7 @@ __global__ void __launch_bounds__(kSThreads, 2) linear_stream_kernel(const __gri
       issue();
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const uint4 q = *reinterpret_cast<const uint4*>(z[t] + 512 * s);
+        const uint4 q = *reinterpret_cast<const uint4*>(z[t] + 64 * kSWarps * s);
         mma_16x8x32(d[t], a.x, b.x, a.y, b.y, q.x, q.y);
         mma_16x8x32(d[t], a.z, b.z, a.w, b.w, q.z, q.w);
       }
@@ -182,7 +184,7 @@ __global__ void __launch_bounds__(kSThreads, 2) linear_stream_kernel(const __gri
 #pragma unroll
       for (int j = 0; j < 4; ++j) atomicAdd(red + 32 * (4 * t + j) + lane, d[t][j]);
     __syncthreads();
-    for (int t = tid >> 4; t < 8 * NT; t += 16) {
+    for (int t = tid >> 4; t < 8 * NT; t += kSThreads / 16) {
       const int row = tid & 15, at = 32 * (4 * (t >> 3) + (t & 1) + 2 * (row >> 3)) + 4 * (row & 7) + ((t & 7) >> 1);
       const int sum = red[at];
       red[at] = 0;
@@ -203,7 +205,8 @@ template <int NT, int kGrid>
 int launch_stream(StreamParams p, cudaStream_t s) {
   p.red_at = kSWarps * Ring<kGrid, kSDepth>::kBytes;
   p.codes_at = p.red_at + 512 * NT;
-  const int dyn = p.codes_at + p.M * p.pitch;
+  int dyn = p.codes_at + p.M * p.pitch;
+  if (dyn < kSLeast) dyn = kSLeast;
   static std::atomic<bool> set[kMaxDevices];
   const int dev = current_device();
   if (dev < 0 || !set[dev].load(std::memory_order_relaxed)) {
@@ -211,7 +214,7 @@ int launch_stream(StreamParams p, cudaStream_t s) {
     if (rc != Q8_OK) return rc;
     if (dev >= 0) set[dev].store(true, std::memory_order_relaxed);
   }
-  const int at_once = sm_count() * (dyn <= 110 * 1024 ? 2 : 1);
+  const int at_once = sm_count();
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(p.tiles < at_once ? p.tiles : at_once));
   cfg.blockDim = dim3(kSThreads);
@@ -239,7 +242,8 @@ bool linear_stream_fits(const LinearArgs& a) {
   return a.M <= kStreamTokens && kSWarps * kSDepth * 1280 + 512 * 4 + (long long)a.M * staged_pitch(steps) <= kSSmem;
 }
 
-// 4096 -> 4096: one token 4.1 us (5.2 from bf16), 8 tokens 5.8; 4096 -> 11008: 11.2 and 15.0; 16 tokens 1024 -> 1024: 3.0.
+// 4096 -> 4096: one token 4.6 us (5.2 from bf16), 8 tokens 5.8; 4096 -> 11008: 9.8, 4 tokens 10.3, 8 tokens 15.0; 16 tokens
+// 1024 -> 1024: 3.0.
 double linear_stream_us(const LinearArgs& a) { return 2.3 + 1e-6 * a.C * a.K * (0.12 + 0.0165 * a.M); }
 
 int launch_linear_stream(const LinearArgs& a) {

@@ -41,10 +41,10 @@ constexpr int kMaxExperts = 1024; // a bit of a lane's word each
 // Warps of a block, by the eights of columns of its kernel: with many columns a warp needs more than 128 registers.
 __host__ __device__ constexpr int warps_of(int nt) { return nt > 2 ? 8 : 16; }
 // Steps of 16 x 64 bytes in a warp's ring: 80 KiB of weights on their way to an SM in phase one (64 with many tokens, whose
-// digits take the room), 128 KiB in phase two, whose items are shorter and have more to wait for.  (kGrid 1: a step takes 1280
-// bytes.)
+// digits take the room), 64 or 48 in phase two, whose items are short: a ring longer than an item holds empty slots, and with few
+// tokens the room is better spent on digits (2 tokens, 4096 x 2048: 37 us, with 128 KiB 43 us; 32 to 128 KiB within 3 % else).
 __host__ __device__ constexpr int depth1_of(int nt) { return (nt > 2 ? 64 : 80) / warps_of(nt); }
-__host__ __device__ constexpr int depth2_of(int nt, int step_bytes) { return (step_bytes == 1024 ? 128 : 96) / warps_of(nt); }
+__host__ __device__ constexpr int depth2_of(int nt) { return (nt > 2 ? 48 : 64) / warps_of(nt); }
 constexpr float kDigitMax = 2139062016.0f;  // the largest fp32 number below 127 (256^3 + 256^2 + 256 + 1)
 // Tickets: blocks and items of phase one, of phase two, rows to be made digits, tiles to be added up; then how many items of
 // phase one, rows and items of phase two are done.  Each on a line of its own: who waits for one does not slow the others.
@@ -491,7 +491,7 @@ struct MoeShared {
     if (digits_at < acc_at + 8 * T * E) digits_at = acc_at + 8 * T * E;
     const int all = 4 * T * staged_pitch(steps);
     staged = all + kOverread <= kMoeSmem - digits_at;
-    own_at = rings_at + warps_of(nt) * depth2_of(nt, step_bytes) * step_bytes;
+    own_at = rings_at + warps_of(nt) * depth2_of(nt) * step_bytes;
     room = ((kMoeSmem - kOverread - own_at) / warps_of(nt)) & ~127;
     total = kMoeSmem;
   }
@@ -649,7 +649,7 @@ __global__ void __launch_bounds__(32 * warps_of(NT), 1) moe_experts_kernel(const
   asm volatile("griddepcontrol.wait;" ::: "memory");
   signed char* const digits = reinterpret_cast<signed char*>(smem + lay.digits_at);
   const unsigned char* const ring1 = smem + lay.rings_at + warp * Ring<kGrid, depth1_of(NT)>::kBytes;
-  constexpr int kLater = depth2_of(NT, Ring<kGrid, 1>::kStep);
+  constexpr int kLater = depth2_of(NT);
   const unsigned char* const ring2 = smem + lay.rings_at + warp * Ring<kGrid, kLater>::kBytes;
   signed char* const own = reinterpret_cast<signed char*>(smem + lay.own_at) + warp * lay.room;
   const int x_staged = staged_pitch(p.steps);
