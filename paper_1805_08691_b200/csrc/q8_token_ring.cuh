@@ -22,8 +22,10 @@ struct Rows {
   int left;
 };
 
-// A warp's ring of kDepth steps.  kGrid: 16 or 8, the alignment of every row, or 1: rows anywhere, copied as aligned words each of which holds
-// a byte of the row and put together when they are read.
+// A warp's ring of kDepth steps.  kGrid: 16 or 8, the alignment of every row, or 1: rows anywhere.  Then a step of a row is the
+// five aligned chunks of 16 bytes that its 64 bytes lie in; a lane copies one of them (the fourth the fifth as well), in as far
+// as the row reaches, and what it reads belongs to two lanes.  (As five words a lane, three times as many copies: 3 tokens,
+// 3313 x 1280, 148 us.)  What lies in a step before or behind the bytes of the row does not matter: the codes there are zero.
 template <int kGrid, int kDepth>
 struct Ring {
   static constexpr int kStep = kGrid == 1 ? 1280 : 1024, kHalf = kStep / 2, kBytes = kDepth * kStep;
@@ -32,41 +34,44 @@ struct Ring {
   int slot;                 // bytes to the slot of the next step, in use and then free: the ring is always full, if only of
                             // groups without copies, so that a group of copies is a slot
   __device__ __forceinline__ void init(const unsigned char* ring, int lane) {
-    at = ring + (kGrid == 1 ? 4 : 16) * lane;
+    at = ring + (kGrid == 1 ? 80 * (lane >> 2) + 16 * (lane & 3) : 16 * lane);
     to = (uint32_t)__cvta_generic_to_shared(at);
     slot = 0;
   }
   template <int kBytes>
-  static __device__ __forceinline__ void copy(uint32_t dst, const void* src, bool live) {
-    const int n = live ? kBytes : 0;  // none: zeros
+  static __device__ __forceinline__ void copy(uint32_t dst, const void* src, int n) {  // n bytes of kBytes, zeros behind them
     if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(kBytes), "r"(n) : "memory");
   }
+  // left: bytes of the row from there on
   static __device__ __forceinline__ void copy_row(uint32_t dst, const signed char* row, int left) {
     if constexpr (kGrid == 16) {
-      copy<16>(dst, row, left > 0);
+      copy<16>(dst, row, left > 0 ? 16 : 0);
     } else if constexpr (kGrid == 8) {
-      copy<8>(dst, row, left > 0);
-      copy<8>(dst + 8, row + 8, left > 8);
+      copy<8>(dst, row, left > 0 ? 8 : 0);
+      copy<8>(dst + 8, row + 8, left > 8 ? 8 : 0);
     } else {
-      const int m = (int)((unsigned long long)row & 3ull);
-#pragma unroll
-      for (int k = 0; k < 5; ++k) copy<4>(dst + 128 * k, row - m + 4 * k, 4 * k - m < left && (k < 4 || m > 0));
+      const int m = (int)((unsigned long long)row & 15ull), n = left + m;
+      copy<16>(dst, row - m, min(max(n, 0), 16));
+      if ((threadIdx.x & 3) == 3) copy<16>(dst + 16, row - m + 16, min(max(n - 16, 0), 16));
     }
   }
   static __device__ __forceinline__ uint4 read_row(const unsigned char* src, const signed char* row) {
     if constexpr (kGrid != 1) {
       return *reinterpret_cast<const uint4*>(src);
     } else {
-      const int m = 8 * (int)((unsigned long long)row & 3ull);
+      const int m = (int)((unsigned long long)row & 15ull), shift = 8 * (m & 3);
+      const unsigned* w = reinterpret_cast<const unsigned*>(src + (m & 12));
       unsigned u[5];
 #pragma unroll
-      for (int k = 0; k < 5; ++k) u[k] = *reinterpret_cast<const unsigned*>(src + 128 * k);
-      return make_uint4(__funnelshift_r(u[0], u[1], m), __funnelshift_r(u[1], u[2], m), __funnelshift_r(u[2], u[3], m), __funnelshift_r(u[3], u[4], m));
+      for (int k = 0; k < 5; ++k) u[k] = w[k];
+      return make_uint4(__funnelshift_r(u[0], u[1], shift), __funnelshift_r(u[1], u[2], shift), __funnelshift_r(u[2], u[3], shift),
+                        __funnelshift_r(u[3], u[4], shift));
     }
   }
   // The step at r into the present slot (live: there is one), and on to the next slot.
   __device__ __forceinline__ void put(Rows& r, bool live) {
+    if constexpr (kGrid == 1) __syncwarp();  // (the slot's last step has been read by all lanes)
     if (live) {
       copy_row(to + slot, r.a, r.left);
       copy_row(to + slot + kHalf, r.b, r.left);
@@ -78,7 +83,10 @@ struct Ring {
     slot = slot == (kDepth - 1) * kStep ? 0 : slot + kStep;
   }
   // The step in the present slot, the oldest; a and b have the alignment of its rows.  put() follows.
-  __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory"); }
+  __device__ __forceinline__ void wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+    if constexpr (kGrid == 1) __syncwarp();
+  }
   __device__ __forceinline__ void get(const Rows& r, uint4& a, uint4& b) {
     a = read_row(at + slot, r.a);
     b = read_row(at + slot + kHalf, r.b);
