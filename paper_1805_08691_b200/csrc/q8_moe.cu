@@ -50,7 +50,7 @@ constexpr float kDigitMax = 2139062016.0f;  // the largest fp32 number below 127
 // phase one, rows and items of phase two are done.  Each on a line of its own: who waits for one does not slow the others.
 enum { kLine = 32, kBlocks1 = 0, kItems1 = kLine, kBlocks2 = 2 * kLine, kItems2 = 3 * kLine, kRows = 4 * kLine, kTiles = 5 * kLine, kDone1 = 6 * kLine,
        kDoneRows = 7 * kLine, kDone2 = 8 * kLine, kCounters = 9 * kLine };
-constexpr int kDirectSteps = 32; // tokens times steps up to which the readers of inner activations make their digits themselves
+constexpr int kDirectTokens = 4, kDirectSteps = 32; // tokens, and tokens times steps, up to which readers of inner activations make their digits themselves
 constexpr unsigned kTimeoutMoe = 32u;
 constexpr unsigned long long kMoeWaitNs = 2000000000ull;
 
@@ -580,8 +580,9 @@ struct Down {
     // digits made here, in the warp's own shared memory
     const int pitch = staged_pitch(n), len = 64 * n;
     __syncwarp();  // (all lanes have read what was there)
+    const unsigned top = lane < count ? __ldcg(largest + first + lane) : 0u;
     for (int r = 0; r < count; ++r) {
-      const DigitScale scale = digit_scale(__ldcg(largest + first + r));
+      const DigitScale scale = digit_scale(__shfl_sync(0xffffffffu, top, r));
 #pragma unroll 8
       for (int c = 4 * lane; c < len; c += 128) {
         unsigned d[4];
@@ -607,20 +608,20 @@ struct Down {
     if (c < p.C) out[0] = __fmul_rn(w, __fmul_rn(__fmul_rn(low, f), s.x));
     if (c + 8 < p.C) out[8] = __fmul_rn(w, __fmul_rn(__fmul_rn(high, f), s.y));
   }
-  // The results of a tile, by a warp.
-  __device__ __forceinline__ void add_up(int t, int lane) const {
+  // The results of two tokens in a tile, by a warp.
+  __device__ __forceinline__ void add_up(int t, int pair, int lane) const {
     const int c = 16 * t + (lane & 15);
     if (c >= p.C) return;
-    for (int token = lane >> 4; token < p.T; token += 2) {
-      const int* rows = ch.row_of + token * p.k;
-      float y = 0.0f;
+    const int token = 2 * pair + (lane >> 4);
+    if (token >= p.T) return;
+    const int* rows = ch.row_of + token * p.k;
+    float y = 0.0f;
 #pragma unroll 8
-      for (int j = 0; j < p.k; ++j) y = __fadd_rn(y, __ldcg(p.part + (size_t)rows[j] * p.C + c));
-      const long long at = (long long)token * p.ldy + c;
-      if (p.x_type == Q8_F32) static_cast<float*>(p.y)[at] = y;
-      else if (p.x_type == Q8_F16) static_cast<__half*>(p.y)[at] = __float2half_rn(y);
-      else static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(y);
-    }
+    for (int j = 0; j < p.k; ++j) y = __fadd_rn(y, __ldcg(p.part + (size_t)rows[j] * p.C + c));
+    const long long at = (long long)token * p.ldy + c;
+    if (p.x_type == Q8_F32) static_cast<float*>(p.y)[at] = y;
+    else if (p.x_type == Q8_F16) static_cast<__half*>(p.y)[at] = __float2half_rn(y);
+    else static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(y);
   }
 };
 
@@ -781,10 +782,12 @@ __global__ void __launch_bounds__(32 * warps_of(NT), 1) moe_experts_kernel(const
   __syncthreads();
   const Down job{p, ch, largest, &p.sync[p.direct ? kDone1 : kDoneRows], (unsigned)(p.direct ? items1 : lay.rows), &s_known, &gave_up, own};
   run_phase<NT, kGrid, kLater>(job, items2, (p.I + 63) >> 6, p.ks[1], &p.sync[kBlocks2], &p.sync[kDone2], s_block[1], s_next, acc, ring2, lane, warp);
-  // ---- the results, a warp a tile of sixteen channels
-  for (int t; (t = draw(&p.sync[kTiles])) < p.tiles;) {
+  // ---- the results, a warp sixteen channels of two tokens
+  const int pairs = (p.T + 1) >> 1;
+  for (int u; (u = draw(&p.sync[kTiles])) < p.tiles * pairs;) {
     if (!wait_counted(&p.sync[kDone2], (unsigned)items2, &gave_up, p.status)) break;
-    job.add_up(t, lane);
+    const int t = u / pairs;
+    job.add_up(t, u - t * pairs, lane);
   }
 }
 
@@ -946,7 +949,7 @@ int q8_moe(const q8_moe_desc* d, const void* x, const float* router, const int8_
     p.ks[0] = warps_per_item(chosen * p.unit_blocks, p.steps, warps);
     p.ks[1] = warps_per_item(chosen * p.tiles, (p.I + 63) / 64, warps);
     const int run = ((p.I + 63) / 64 + p.ks[1] - 1) / p.ks[1];  // steps of a warp
-    p.direct = p.T * run <= kDirectSteps ? 4 * p.T * staged_pitch(run) : 0;
+    p.direct = p.T <= kDirectTokens && p.T * run <= kDirectSteps ? 4 * p.T * staged_pitch(run) : 0;
     p.x = static_cast<const char*>(x) + (size_t)t0 * p.ldx * e;
     p.y = static_cast<char*>(y) + (size_t)t0 * p.ldy * e;
     p.ids = ids ? ids + (size_t)t0 * p.k : nullptr;
