@@ -45,6 +45,8 @@ __host__ __device__ constexpr int warps_of(int nt) { return nt > 2 ? 8 : 16; }
 // tokens the room is better spent on digits (2 tokens, 4096 x 2048: 37 us, with 128 KiB 43 us; 32 to 128 KiB within 3 % else).
 __host__ __device__ constexpr int depth1_of(int nt) { return (nt > 2 ? 64 : 80) / warps_of(nt); }
 __host__ __device__ constexpr int depth2_of(int nt) { return (nt > 2 ? 48 : 64) / warps_of(nt); }
+// Steps of digits in the hands of a warp with N columns, besides as many on their way.
+__host__ __device__ constexpr int ahead_of(int nt, int n) { return n == 2 && nt > 2 ? 4 : (n <= 4 ? 2 : 1); }
 constexpr float kDigitMax = 2139062016.0f;  // the largest fp32 number below 127 (256^3 + 256^2 + 256 + 1)
 // Tickets: blocks and items of phase one, of phase two, rows to be made digits, tiles to be added up; then how many items of
 // phase one, rows and items of phase two are done.  Each on a line of its own: who waits for one does not slow the others.
@@ -321,8 +323,8 @@ __device__ __forceinline__ void make_digits(const MoeParams& p, int row, unsigne
 }
 
 // All items of a phase, by groups of ks warps.  J says what an item is: rows() its weights, scales() the factors of this lane's
-// two rows, columns() its digits, finish() takes the sums of a token with these rows (all lanes call it).  Behind the last
-// item, `done` has gone up by the items of this call's warps.
+// two rows, columns() its digits, token() what the factor of a token is made of, finish() takes the sums of a token with these
+// rows (all lanes call it).  Behind the last item, `done` has gone up by the items of this call's warps.
 //
 // Block b begins with the items b + blocks * group, and draws those behind them by tickets.  b is drawn too, so that blocks
 // that run have the first numbers; a group that finds no more tickets takes over the first items of a block that has not
@@ -373,9 +375,12 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
 #pragma unroll
         for (int t = 0; t < N; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0;
         job.columns(cur, count, s0, n, lane, z);
+        unsigned f[N];  // of this lane's tokens, on their way until the item's end
+#pragma unroll
+        for (int t = 0; t < N; ++t) f[t] = job.token(cur, min(2 * t + (i >> 1), count - 1));
         // digits two steps ahead: from L2 they take as long as a few steps of the scheduler's other warps.  (Reads behind an
         // item's last step stay inside the workspace or shared memory and are not used.)
-        constexpr int A = N <= 4 ? 2 : 1;
+        constexpr int A = ahead_of(NT, N);
         uint4 q[2][A][N];
         auto fetch = [&](int half) {
 #pragma unroll
@@ -440,7 +445,7 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
             a = __fmaf_rn(a, 65536.0f, __shfl_xor_sync(0xffffffffu, a, 1));
             b = __fmaf_rn(b, 65536.0f, __shfl_xor_sync(0xffffffffu, b, 1));
             const int token = 2 * t + (i >> 1);
-            job.finish(cur, token, g, !(i & 1) && token < count, a, b, scales);
+            job.finish(cur, token, g, !(i & 1) && token < count, a, b, scales, f[t]);
           }
         }
       };
@@ -478,7 +483,7 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
 // Shared memory of a block: lists of rows; partial sums of warps that share items; then the warps' rings and digits, the tokens'
 // in phase one if there is room, a warp's own in phase two.  The logits' keys [T][E] lie over sums and rings until the choice
 // is made.
-constexpr int kOverread = 512;     // bytes behind digits that may be read, and are not used
+constexpr int kOverread = 64 * (10 + 2 * 4);  // bytes behind digits that may be read, and are not used: the slots of a ring and twice the steps ahead
 constexpr int kMoeSmem = 226 * 1024;
 struct MoeShared {
   int rows, chosen, acc_at, rings_at, digits_at, staged, own_at, room, total;
@@ -528,11 +533,12 @@ struct GateUp {
     const float* s = p.sgu + (size_t)ch.expert[a] * 2 * p.I + i;
     return make_float2(__ldg(s), __ldg(s + p.I));
   }
-  __device__ __forceinline__ void finish(int item, int r, int u, bool live, float gate, float up, float2 s) const {
+  __device__ __forceinline__ unsigned token(int item, int r) const { return __float_as_uint(__ldg(p.x_factor + ch.row_token[ch.first[expert(item)] + r])); }
+  __device__ __forceinline__ void finish(int item, int r, int u, bool live, float gate, float up, float2 s, unsigned factor) const {
     const int a = expert(item), i = (item - a * p.unit_blocks) * 8 + u, row = ch.first[a] + r;
     unsigned m = 0;
     if (live && i < p.I) {
-      const float f = p.x_factor[ch.row_token[row]];
+      const float f = __uint_as_float(factor);
       const float g = __fmul_rn(__fmul_rn(gate, f), s.x), v = __fmul_rn(__fmul_rn(up, f), s.y);
       const float h = __fmul_rn(__fdividef(g, __fadd_rn(1.0f, expf(-g))), v);  // (divided within 2 ulp, or 0 for gates below -87)
       p.h[(size_t)row * p.h_pitch + i] = h;
@@ -600,10 +606,11 @@ struct Down {
     const float* s = p.sd + (size_t)ch.expert[a] * p.C;
     return make_float2(__ldg(s + min(c, p.C - 1)), __ldg(s + min(c + 8, p.C - 1)));
   }
-  __device__ __forceinline__ void finish(int item, int r, int u, bool live, float low, float high, float2 s) const {
+  __device__ __forceinline__ unsigned token(int item, int r) const { return __ldcg(largest + ch.first[expert(item)] + r); }
+  __device__ __forceinline__ void finish(int item, int r, int u, bool live, float low, float high, float2 s, unsigned top) const {
     if (!live) return;
     const int a = expert(item), c = 16 * (item - a * p.tiles) + u, row = ch.first[a] + r;
-    const float f = digit_scale(__ldcg(largest + row)).factor, w = ch.prob[row];
+    const float f = digit_scale(top).factor, w = ch.prob[row];
     float* out = p.part + (size_t)row * p.C + c;
     if (c < p.C) out[0] = __fmul_rn(w, __fmul_rn(__fmul_rn(low, f), s.x));
     if (c + 8 < p.C) out[8] = __fmul_rn(w, __fmul_rn(__fmul_rn(high, f), s.y));
