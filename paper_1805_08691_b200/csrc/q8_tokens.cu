@@ -1,11 +1,14 @@
 // Codes and factors of tokens (q8_quantize_tokens) and the way back (q8_dequantize_tokens).
 //
-// Bound by memory.  A team of threads (a warp, or a block of 128 or 512) takes a token and holds its values in registers between
-// the maximum and the codes, so that they are read from memory once; what a team cannot hold is read a second time, from L2.
-// A thread takes 16 bytes of a row at a time where rows lie on the 16-byte grid, else four values.  Teams are as large as
-// leaves a thread about four of these (64 bytes in flight each, 128 KiB an SM), and with fewer tokens than that occupies the
-// GPU large enough for one each: one token of 4096 values is then a few microseconds of latency and nothing else.
-// 8192 x 4096 bf16: 47 -> FIGQ us to codes (FIGQB TB/s), FIGD us back (FIGDB TB/s); the first form here, a block a token that
+// Bound by memory.  A team of threads (a warp, or a block of 128, 256 or 512) takes a token and holds its values in registers
+// between the maximum and the codes, so that they are read from memory once; what a team cannot hold is read a second time,
+// from L2.  Teams are as large as leaves a thread about four pieces of 16 bytes (64 bytes in flight each), and with fewer tokens
+// than that occupies the GPU large enough for one each: one token of 4096 values is then 1.6 us of latency and nothing else.
+// Registers are held to what five blocks of 256 threads leave (8192 x 4096 f32: 33 us, with 512 threads a row 45).
+// Rows off the 16-byte grid: four 16-bit values that adjoin, or four fp32 values as far apart as the team is large, so that a
+// warp's addresses adjoin (1000 x 2051 f32: 5.0 us against 5.6; 8192 x 2678 f16: 31 us against 34 the other way round), and so
+// on the way back for all types (8192 x 2678 f16: 21 us against 26).
+// 8192 x 4096 bf16: 22 us to codes (4.6 TB/s of 6.5 measured), 19 us back (5.3 TB/s); the first form here, a block a token that
 // read its row twice, value by value, 73 us for both.
 #include "q8_token_common.cuh"
 
@@ -14,10 +17,11 @@ namespace {
 
 constexpr int kHeld = 4;  // chunks a thread holds
 
-// Sixteen bytes of a row (V values), or four values where rows do not lie on that grid; those from C on are zero.
-template <typename T, bool kVec>
+// Sixteen bytes of a row (V values), or four values; those from C on are zero.
+template <typename T, bool kVec, int kTeam>
 struct Chunk {
   static constexpr int V = kVec ? 16 / (int)sizeof(T) : 4;
+  static constexpr int kStep = kVec || sizeof(T) == 2 ? 1 : kTeam;  // from value to value
   unsigned w[V * sizeof(T) / 4];
   __device__ __forceinline__ void load(const T* row, size_t c, size_t C) {
     if (kVec && c + V <= C) {
@@ -25,11 +29,11 @@ struct Chunk {
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const bool live = c + j < C;
+        const bool live = c + j * kStep < C;
         if constexpr (sizeof(T) == 4) {
-          w[j] = live ? reinterpret_cast<const unsigned*>(row)[c + j] : 0u;
+          w[j] = live ? reinterpret_cast<const unsigned*>(row)[c + j * kStep] : 0u;
         } else {
-          const unsigned h = live ? reinterpret_cast<const unsigned short*>(row)[c + j] : 0u;
+          const unsigned h = live ? reinterpret_cast<const unsigned short*>(row)[c + j * kStep] : 0u;
           w[j / 2] = j & 1 ? w[j / 2] | h << 16 : h;
         }
       }
@@ -43,8 +47,8 @@ struct Chunk {
       else m = max_two(m, w[j]);
     }
   }
-  // z: the row's codes; aligned: V codes can be written at once
-  __device__ __forceinline__ void store(signed char* z, size_t c, size_t C, const TokenFactor& f, bool aligned) const {
+  // z: the row's codes
+  __device__ __forceinline__ void store(signed char* z, size_t c, size_t C, const TokenFactor& f) const {
     unsigned o[V / 4];
 #pragma unroll
     for (int j = 0; j < V / 4; ++j) {
@@ -58,13 +62,13 @@ struct Chunk {
       }
       o[j] = f.finite ? codes_4(v, f) : 0u;
     }
-    if (aligned && c + V <= C) {
+    if (kVec && c + V <= C) {
       if constexpr (V == 8) *reinterpret_cast<uint2*>(z + c) = make_uint2(o[0], o[1]);
       else *reinterpret_cast<unsigned*>(z + c) = o[0];
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j)
-        if (c + j < C) z[c + j] = (signed char)(o[j / 4] >> (8 * (j & 3)));
+        if (c + j * kStep < C) z[c + j * kStep] = (signed char)(o[j / 4] >> (8 * (j & 3)));
     }
   }
 };
@@ -81,9 +85,9 @@ __device__ __forceinline__ unsigned as_fp32_bits(unsigned m) {  // of a maximum 
 
 // Teams of kTeam threads, a token each.  kTeam 32: eight tokens a block.
 template <typename T, bool kVec, int kTeam>
-__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam) quantize_tokens_kernel(const T* __restrict__ x, size_t tokens, size_t C, size_t ldx,
-                                                                                    signed char* __restrict__ z, size_t ldz, float* __restrict__ scale, int z_aligned) {
-  constexpr int V = Chunk<T, kVec>::V;
+__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? (sizeof(T) == 4 ? 3 : 2) : (kTeam == 128 ? 10 : 5)) quantize_tokens_kernel(const T* __restrict__ x, size_t tokens, size_t C, size_t ldx,
+                                                                                    signed char* __restrict__ z, size_t ldz, float* __restrict__ scale) {
+  using Part = Chunk<T, kVec, kTeam>;
   __shared__ unsigned part[kTeam / 32];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -92,18 +96,18 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam) quantize_tokens_ker
   if (kTeam == 32 && t >= tokens) return;
   const T* row = x + t * ldx;
   signed char* out = z + t * ldz;
-  Chunk<T, kVec> held[kHeld];
+  constexpr int kTurn = kTeam * Part::V;
+  const size_t c0 = (size_t)tid * (Part::kStep == 1 ? Part::V : 1);
+  Part held[kHeld];
   unsigned m = 0;
 #pragma unroll
-  for (int j = 0; j < kHeld; ++j) {
-    const size_t c = (size_t)(tid + j * kTeam) * V;
-    if (c < C) held[j].load(row, c, C);
-  }
+  for (int j = 0; j < kHeld; ++j)
+    if (c0 + j * kTurn < C) held[j].load(row, c0 + j * kTurn, C);
 #pragma unroll
   for (int j = 0; j < kHeld; ++j)
-    if ((size_t)(tid + j * kTeam) * V < C) held[j].max_into(m);
-  for (size_t c = (size_t)(tid + kHeld * kTeam) * V; c < C; c += (size_t)kTeam * V) {
-    Chunk<T, kVec> again;
+    if (c0 + j * kTurn < C) held[j].max_into(m);
+  for (size_t c = c0 + kHeld * kTurn; c < C; c += kTurn) {
+    Part again;
     again.load(row, c, C);
     again.max_into(m);
   }
@@ -117,18 +121,16 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam) quantize_tokens_ker
   const TokenFactor f = token_factor(m);
   if (tid == 0) scale[t] = f.s;
 #pragma unroll
-  for (int j = 0; j < kHeld; ++j) {
-    const size_t c = (size_t)(tid + j * kTeam) * V;
-    if (c < C) held[j].store(out, c, C, f, z_aligned);
-  }
-  for (size_t c = (size_t)(tid + kHeld * kTeam) * V; c < C; c += (size_t)kTeam * V) {
-    Chunk<T, kVec> again;
+  for (int j = 0; j < kHeld; ++j)
+    if (c0 + j * kTurn < C) held[j].store(out, c0 + j * kTurn, C, f);
+  for (size_t c = c0 + kHeld * kTurn; c < C; c += kTurn) {
+    Part again;
     again.load(row, c, C);
-    again.store(out, c, C, f, z_aligned);
+    again.store(out, c, C, f);
   }
 }
 
-// Sixteen codes a thread and turn where rows lie on the 16-byte grid, else four.
+// Sixteen codes a thread and turn where rows lie on the 16-byte grid, else four kTeam apart.
 template <typename T, bool kVec, int kTeam>
 __global__ void __launch_bounds__(256) dequantize_tokens_kernel(const signed char* __restrict__ z, size_t tokens, size_t C, size_t ldz,
                                                                 const float* __restrict__ scale, T* __restrict__ r, size_t ldr) {
@@ -140,7 +142,8 @@ __global__ void __launch_bounds__(256) dequantize_tokens_kernel(const signed cha
   const float s = scale[t];
   const signed char* in = z + t * ldz;
   T* out = r + t * ldr;
-  for (size_t c = (size_t)(threadIdx.x % kTeam) * V; c < C; c += (size_t)kTeam * V) {
+  constexpr int kStep = kVec ? 1 : kTeam;
+  for (size_t c = (size_t)(threadIdx.x % kTeam) * (kVec ? V : 1); c < C; c += (size_t)kTeam * V) {
     if (kVec && c + V <= C) {
       const uint4 w = __ldg(reinterpret_cast<const uint4*>(in + c));
       const unsigned u[4] = {w.x, w.y, w.z, w.w};
@@ -155,10 +158,15 @@ __global__ void __launch_bounds__(256) dequantize_tokens_kernel(const signed cha
           reinterpret_cast<uint4*>(out + c)[j / 2] = make_uint4(pack_two<T>(v[0], v[1]), pack_two<T>(v[2], v[3]), pack_two<T>(x[0], x[1]), pack_two<T>(x[2], x[3]));
         }
       }
+    } else if (kVec) {
+      for (int j = 0; c + j < C; ++j) out[c + j] = from_f32<T>(__fmul_rn(s, (float)in[c + j]));
     } else {
+      signed char v[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = c + j * kStep < C ? in[c + j * kStep] : (signed char)0;
 #pragma unroll
       for (int j = 0; j < V; ++j)
-        if (c + j < C) out[c + j] = from_f32<T>(__fmul_rn(s, (float)in[c + j]));
+        if (c + j * kStep < C) out[c + j * kStep] = from_f32<T>(__fmul_rn(s, (float)v[j]));
     }
   }
 }
@@ -181,8 +189,7 @@ constexpr size_t kMostTokens = 0x7fffffff;  // of a launch
 
 template <typename T, bool kVec>
 int quantize_as(const T* x, size_t tokens, size_t C, size_t ldx, signed char* z, size_t ldz, float* scale, cudaStream_t s) {
-  constexpr int V = Chunk<T, kVec>::V;
-  const int z_aligned = aligned_to(z, V) && ldz % V == 0;
+  constexpr int V = Chunk<T, kVec, 32>::V;
   const size_t chunks = (C + V - 1) / V;
   // chunks a thread: about four, one where that leaves fewer than two blocks an SM
   const size_t want = tokens < (size_t)2 * sm_count() ? chunks : (chunks + 3) / 4;
@@ -191,9 +198,10 @@ int quantize_as(const T* x, size_t tokens, size_t C, size_t ldx, signed char* z,
     const T* xt = x + t0 * ldx;
     signed char* zt = z + t0 * ldz;
     int rc;
-    if (want <= 32) rc = launch_dependent("quantize_tokens_kernel", quantize_tokens_kernel<T, kVec, 32>, (n + 7) / 8, 256, s, xt, n, C, ldx, zt, ldz, scale + t0, z_aligned);
-    else if (want <= 192) rc = launch_dependent("quantize_tokens_kernel", quantize_tokens_kernel<T, kVec, 128>, n, 128, s, xt, n, C, ldx, zt, ldz, scale + t0, z_aligned);
-    else rc = launch_dependent("quantize_tokens_kernel", quantize_tokens_kernel<T, kVec, 512>, n, 512, s, xt, n, C, ldx, zt, ldz, scale + t0, z_aligned);
+    if (want <= 32) rc = launch_dependent("quantize_tokens_kernel", quantize_tokens_kernel<T, kVec, 32>, (n + 7) / 8, 256, s, xt, n, C, ldx, zt, ldz, scale + t0);
+    else if (want <= 192) rc = launch_dependent("quantize_tokens_kernel", quantize_tokens_kernel<T, kVec, 128>, n, 128, s, xt, n, C, ldx, zt, ldz, scale + t0);
+    else if (want <= 320) rc = launch_dependent("quantize_tokens_kernel", quantize_tokens_kernel<T, kVec, 256>, n, 256, s, xt, n, C, ldx, zt, ldz, scale + t0);
+    else rc = launch_dependent("quantize_tokens_kernel", quantize_tokens_kernel<T, kVec, 512>, n, 512, s, xt, n, C, ldx, zt, ldz, scale + t0);
     if (rc != Q8_OK) return rc;
   }
   return Q8_OK;
@@ -201,7 +209,8 @@ int quantize_as(const T* x, size_t tokens, size_t C, size_t ldx, signed char* z,
 template <typename T>
 int quantize_any(const void* x, size_t tokens, size_t C, size_t ldx, signed char* z, size_t ldz, float* scale, cudaStream_t s) {
   const T* p = static_cast<const T*>(x);
-  if (aligned16(x) && ldx * sizeof(T) % 16 == 0) return quantize_as<T, true>(p, tokens, C, ldx, z, ldz, scale, s);
+  constexpr size_t V = Chunk<T, true, 32>::V;
+  if (aligned16(x) && ldx % V == 0 && aligned_to(z, V) && ldz % V == 0) return quantize_as<T, true>(p, tokens, C, ldx, z, ldz, scale, s);
   return quantize_as<T, false>(p, tokens, C, ldx, z, ldz, scale, s);
 }
 
