@@ -90,6 +90,50 @@ def prepare_conv(w, b, in_shape, q_x, q_y, x_type=q8.Q8_U8, y_type=q8.Q8_U8, rel
     return QuantConv(desc, w_q, b_q, scale, q_w, q_x, q_y, res_scale)
 
 
+@dataclass
+class QuantLinear:
+    """One linear layer ready to run: s8 weights [K, C] and their factors, fp32 bias, type of the results."""
+    w_q: torch.Tensor
+    w_scale: torch.Tensor
+    bias: Optional[torch.Tensor]
+    out_type: int
+
+    def __call__(self, x, x_scale=None, out=None, workspace=None):
+        """x: activations, quantized here token by token, or codes with x_scale, a factor for each token."""
+        return q8.q8_linear(x, self.w_q, self.w_scale, x_scale, self.bias, self.out_type, out, workspace)
+
+
+def prepare_linear(w, bias=None, out_type=q8.Q8_BF16) -> QuantLinear:
+    """w: fp32, fp16 or bf16 weights [K, C] on the device, bias: [K] or None.  Each output channel has its own factor, which
+    rounds as that of a token does: max|w[k]| / 127."""
+    w_q, w_scale = q8.q8_quantize_tokens(w)
+    return QuantLinear(w_q, w_scale, None if bias is None else bias.float().contiguous(), out_type)
+
+
+@dataclass
+class QuantExperts:
+    """A mixture-of-experts layer ready to run: fp32 router, s8 weights of the experts and their factors."""
+    router: torch.Tensor
+    w_gate_up: torch.Tensor
+    s_gate_up: torch.Tensor
+    w_down: torch.Tensor
+    s_down: torch.Tensor
+    top_k: int
+    renormalize: bool
+
+    def __call__(self, x, out=None, workspace=None):
+        """Returns (y, the chosen experts, their weights)."""
+        return q8.q8_moe(x, self.router, self.w_gate_up, self.s_gate_up, self.w_down, self.s_down, self.top_k, self.renormalize,
+                         out, None, None, workspace)
+
+
+def prepare_experts(router, w_gate_up, w_down, top_k, renormalize=True) -> QuantExperts:
+    """router [E, C]; fp32, fp16 or bf16 weights: w_gate_up [E, 2 I, C], gate rows first, and w_down [E, C, I]."""
+    gate_up = q8.q8_quantize_tokens(w_gate_up, out=torch.empty(w_gate_up.shape, dtype=torch.int8, device=w_gate_up.device))
+    down = q8.q8_quantize_tokens(w_down, out=torch.empty(w_down.shape, dtype=torch.int8, device=w_down.device))
+    return QuantExperts(router.float().contiguous(), *gate_up, *down, top_k, renormalize)
+
+
 def fused_pair(first: QuantConv, second: QuantConv, x_q, residual=None, out=None):
     """`first` followed by the 1x1 layer `second` in one launch; the tensor between them is never written."""
     return q8.q8_conv2d_then_1x1(first.desc, second.desc, x_q, first.w_q, first.b_q, first.scale, second.w_q, second.b_q,

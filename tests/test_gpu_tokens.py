@@ -121,6 +121,13 @@ def check_linear(y, z, s, w, ws, bias):
     info = torch.finfo(y.dtype)
     tol = 3 * 2.0 ** -24 * exact.abs() * 1.000001 + (2.0 ** -24 * total.abs() if bias is not None else 0)
     tol = tol + (total.abs() + tol) * (info.eps / 2 if y.dtype != torch.float32 else 0) + info.smallest_normal * info.eps
+    if y.dtype == torch.float16:
+        # the last fp16 number is 2^16 - 2^5; from half a step above it on, 2^16 - 2^4, values round to infinity
+        bound = tol - total.abs() * info.eps / 2
+        gone = torch.isinf(y)
+        assert bool((gone == (total.abs() >= 65520))[(total.abs() - 65520).abs() > bound].all())
+        assert bool((torch.sign(y.to(F64)) == torch.sign(total))[gone].all())
+        y, total = torch.where(gone, 0, y), torch.where(gone, 0, total)
     assert bool(((y.to(F64) - total).abs() <= tol).all()), float(((y.to(F64) - total).abs() / tol).max())
 
 
@@ -377,7 +384,133 @@ def test_moe_workspace_contents_do_not_matter(q8):
         q8.q8_moe(x, *experts, 2, workspace=ws[:n - 1])
 
 
+# ------------------------------------------------------------------------------------------------ edges between the kernels
+@pytest.mark.parametrize("C,K", [(512, 384), (1001, 130), (136, 1027)])
+def test_linear_rows_do_not_depend_on_the_batch(q8, C, K):
+    """Sums are exact, so a token's results are the same bits in every batch, whichever kernel takes it."""
+    z, s = q8.q8_quantize_tokens(_acts(80, 300, C))
+    w, ws, bias = _codes(81, K, C), torch.rand(K, device="cuda"), torch.randn(K, generator=_gen(82), device="cuda")
+    want = q8.q8_linear(z, w, ws, x_scale=s, bias=bias, out_type=q8.Q8_F32)
+    check_linear(want, z, s, w, ws, bias)
+    for M in (1, 2, 3, 4, 5, 8, 9, 15, 16, 17, 24, 31, 33, 63, 65, 127, 129, 192, 255, 256, 257, 288):
+        assert torch.equal(q8.q8_linear(z[:M], w, ws, x_scale=s[:M], bias=bias, out_type=q8.Q8_F32), want[:M]), M
+    empty = torch.empty(0, dtype=torch.uint8, device="cuda")
+    assert torch.equal(q8.q8_linear(z, w, ws, x_scale=s, bias=bias, out_type=q8.Q8_F32, workspace=empty), want)
+    q8.q8_read_status()
+
+
+@pytest.mark.parametrize("M", [1, 12, 40, 300])
+@pytest.mark.parametrize("at,ld", [(1, 513), (8, 520), (16, 528), (3, 512)])
+def test_linear_from_any_address(q8, M, at, ld):
+    C, K = 500, 260
+    flat = _codes(83, at + K * ld)
+    w = flat[at:].view(K, ld)[:, :C]
+    x = _codes(84, at + M * ld)[at:].view(M, ld)[:, :C]
+    s, ws = torch.rand(M, device="cuda"), torch.rand(K, device="cuda")
+    y = torch.zeros(at + M * ld, dtype=torch.float16, device="cuda")[at:].view(M, ld)[:, :K]
+    q8.q8_linear(x, w, ws, x_scale=s, out=y)
+    assert torch.equal(y, q8.q8_linear(x.contiguous(), w.contiguous(), ws, x_scale=s, out_type=q8.Q8_F16))
+    check_linear(y, x, s, w, ws, None)
+
+
+@pytest.mark.parametrize("T,C,I,E,k", [(3, 256, 128, 6, 2), (16, 264, 72, 5, 2), (1, 130, 34, 4, 4)])
+def test_moe_from_any_address(q8, T, C, I, E, k):
+    x = _acts(85, T, C, dtype=torch.float16)
+    router, wgu, sgu, wd, sd = _experts(86, C, I, E)
+    want = q8.q8_moe(x, router, wgu, sgu, wd, sd, k)
+    check_moe(want, plain_moe(x, router, wgu, sgu, wd, sd, k, True))
+    for a, b in ((1, 0), (0, 1), (8, 8), (24, 3)):
+        gu = torch.empty(wgu.numel() + a, dtype=torch.int8, device="cuda")[a:].view(wgu.shape).copy_(wgu)
+        down = torch.empty(wd.numel() + b, dtype=torch.int8, device="cuda")[b:].view(wd.shape).copy_(wd)
+        r = torch.empty(router.numel() + 1, device="cuda")[1:].view(router.shape).copy_(router)
+        assert all(torch.equal(p, q) for p, q in zip(q8.q8_moe(x, r, gu, sgu, down, sd, k), want))
+
+
+@pytest.mark.parametrize("T,k,E", [(20, 20, 32), (33, 32, 40), (16, 16, 16), (9, 32, 32)])
+def test_moe_of_many_chosen_experts(q8, T, k, E):
+    C, I = 96, 40
+    x, experts = _acts(87, T, C), _experts(88, C, I, E)
+    for renorm in (True, False):
+        check_moe(q8.q8_moe(x, *experts, k, renormalize=renorm), plain_moe(x, *experts, k, renorm))
+
+
+def test_moe_where_one_expert_takes_all(q8):
+    """Every token chooses the same two experts, others none: sixteen tokens of an item, and experts with nothing to do."""
+    T, C, I, E, k = 16, 320, 200, 48, 2
+    x = _acts(89, T, C).abs()
+    router, *rest = _experts(90, C, I, E)
+    router[:] = -router.abs()
+    router[17] = 1.0
+    router[40] = 2.0
+    got = q8.q8_moe(x, router, *rest, k)
+    assert got[1].tolist() == [[40, 17]] * T
+    check_moe(got, plain_moe(x, router, *rest, k, True))
+
+
+def test_calls_on_two_streams_at_once(q8):
+    """Each call with a workspace of its own; results as one after the other."""
+    T, C, I, E, k = 5, 512, 320, 24, 4
+    xs = [_acts(91 + i, T, C, dtype=torch.bfloat16) for i in range(2)]
+    experts = _experts(93, C, I, E)
+    w, ws = _codes(94, 640, C), torch.rand(640, device="cuda")
+    want = [(q8.q8_moe(x, *experts, k), q8.q8_linear(x, w, ws)) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, (x, stream) in enumerate(zip(xs, streams)):
+            with torch.cuda.stream(stream):
+                got[i].append((q8.q8_moe(x, *experts, k), q8.q8_linear(x, w, ws)))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for moe, y in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(moe, want[i][0])) and torch.equal(y, want[i][1])
+    q8.q8_read_status()
+
+
+def test_two_graphs_share_a_workspace(q8):
+    T, C, I, E, k = 3, 256, 192, 8, 2
+    x, experts = _acts(95, T, C), _experts(96, C, I, E)
+    w, ws = _codes(97, 2048, C), torch.rand(2048, device="cuda")
+    d = q8.q8_moe_desc(0, 0, T, C, I, E, k, q8.Q8_F32, 1, 0)
+    space = torch.empty(max(q8.q8_moe_workspace_bytes(d), 8 << 20), dtype=torch.uint8, device="cuda")
+    graphs, outs = [], []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            y = q8.q8_moe(x, *experts, k, workspace=space)
+            outs.append((*y, q8.q8_linear(y[0], w, ws, workspace=space)))
+        graphs.append(g)
+    for seed in (98, 99):
+        x.copy_(_acts(seed, T, C))
+        for g in graphs:
+            g.replay()
+        want = q8.q8_moe(x, *experts, k)
+        want = (*want, q8.q8_linear(want[0], w, ws))
+        for o in outs:
+            assert all(torch.equal(a, b) for a, b in zip(o, want))
+
+
 # ------------------------------------------------------------------------------------------------ as they are used
+def test_prepared_layers(q8):
+    from paper_1805_08691_b200 import pipeline
+    T, C, I, E, k = 5, 200, 72, 6, 2
+    x = _acts(100, T, C, dtype=torch.bfloat16)
+    w, bias = _acts(101, 130, C, dtype=torch.bfloat16), torch.randn(130, generator=_gen(102), device="cuda")
+    layer = pipeline.prepare_linear(w, bias, q8.Q8_F32)
+    zr, sr = plain_quantize(w)
+    assert np.array_equal(layer.w_q.cpu().numpy(), zr) and np.array_equal(layer.w_scale.cpu().numpy(), sr)
+    z, s = q8.q8_quantize_tokens(x)
+    check_linear(layer(x), z, s, layer.w_q, layer.w_scale, bias)
+    assert torch.equal(layer(z, s), layer(x))
+    g = _gen(103)
+    router, gate_up, down = (torch.randn(*n, generator=g, device="cuda") for n in ((E, C), (E, 2 * I, C), (E, C, I)))
+    experts = pipeline.prepare_experts(router / C ** 0.5, gate_up.half(), down.half(), k, renormalize=False)
+    zr, sr = plain_quantize(down.half())
+    assert np.array_equal(experts.w_down.cpu().numpy(), zr) and np.array_equal(experts.s_down.cpu().numpy(), sr)
+    check_moe(experts(x), plain_moe(x, experts.router, experts.w_gate_up, experts.s_gate_up, experts.w_down, experts.s_down, k, False))
+
+
 def test_a_layer_of_all_of_them(q8):
     """Projection of the activations, its result through the experts, a projection of codes shared by two products."""
     T, C = 6, 256
