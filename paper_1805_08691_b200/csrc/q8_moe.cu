@@ -48,10 +48,11 @@ __host__ __device__ constexpr int depth2_of(int nt) { return (nt > 2 ? 48 : 64) 
 // Steps of digits in the hands of a warp with N columns, besides as many on their way.
 __host__ __device__ constexpr int ahead_of(int nt, int n) { return n == 2 && nt > 2 ? 4 : (n <= 4 ? 2 : 1); }
 constexpr float kDigitMax = 2139062016.0f;  // the largest fp32 number below 127 (256^3 + 256^2 + 256 + 1)
-// Tickets: blocks and items of phase one, of phase two, rows to be made digits, tiles to be added up; then how many items of
-// phase one, rows and items of phase two are done.  Each on a line of its own: who waits for one does not slow the others.
-enum { kLine = 32, kBlocks1 = 0, kItems1 = kLine, kBlocks2 = 2 * kLine, kItems2 = 3 * kLine, kRows = 4 * kLine, kTiles = 5 * kLine, kDone1 = 6 * kLine,
-       kDoneRows = 7 * kLine, kDone2 = 8 * kLine, kCounters = 9 * kLine };
+// Tickets: blocks and items of phase one, of phase two, rows to be made digits; then how many items of phase one and rows are
+// done.  Each on a line of its own: who waits for one does not slow the others.
+enum { kLine = 32, kBlocks1 = 0, kItems1 = kLine, kBlocks2 = 2 * kLine, kItems2 = 3 * kLine, kRows = 4 * kLine, kDone1 = 5 * kLine, kDoneRows = 6 * kLine,
+       kCounters = 7 * kLine };
+constexpr unsigned kAbsent = 0xffffffffu;  // what stands in `part` until a result does (no operation gives this NaN)
 constexpr int kDirectTokens = 4, kDirectSteps = 32; // tokens, and tokens times steps, up to which readers of inner activations make their digits themselves
 constexpr unsigned kTimeoutMoe = 32u;
 constexpr unsigned long long kMoeWaitNs = 2000000000ull;
@@ -146,6 +147,11 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  {
+    uint4* part = reinterpret_cast<uint4*>(p.part);
+    const size_t n = ((size_t)p.T * p.k * p.C + 3) / 4;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) part[i] = make_uint4(kAbsent, kAbsent, kAbsent, kAbsent);
+  }
   if ((int)blockIdx.x < p.T) {  // digits of a token
     const int t = blockIdx.x;
     if (t == 0) for (int i = threadIdx.x; i < kCounters + p.T * p.k; i += 256) p.sync[i] = 0u;
@@ -264,22 +270,23 @@ __device__ __forceinline__ void add_release(unsigned* p, unsigned v) {
   asm volatile("red.relaxed.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }
 
+// Whether a wait that began at t0 (0: begins now) has to end without what it waits for.  All lanes of a warp call it.
+__device__ __noinline__ bool gave_up_in_time(unsigned long long& t0, volatile int* gave_up, unsigned* status) {
+  unsigned long long now;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+  if (t0 == 0) t0 = now;
+  int over = *gave_up;
+  if (now - t0 > kMoeWaitNs) over = 1;
+  if (!__any_sync(0xffffffffu, over)) return false;
+  if ((threadIdx.x & 31) == 0) { *gave_up = 1; atomicOr(status, kTimeoutMoe); }
+  return true;
+}
 // Whether `*counter` reached n in time.  All lanes of a warp call it.
 __device__ __noinline__ bool wait_counted(const unsigned* counter, unsigned n, volatile int* gave_up, unsigned* status) {
   unsigned long long t0 = 0;
   for (unsigned spins = 1;; ++spins) {
     if (__all_sync(0xffffffffu, load_acquire(counter) == n)) return true;
-    if ((spins & 255u) == 0) {
-      unsigned long long now;
-      asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-      if (t0 == 0) t0 = now;
-      int over = *gave_up;
-      if (now - t0 > kMoeWaitNs) over = 1;
-      if (__any_sync(0xffffffffu, over)) {
-        if ((threadIdx.x & 31) == 0) { *gave_up = 1; atomicOr(status, kTimeoutMoe); }
-        return false;
-      }
-    }
+    if ((spins & 255u) == 0 && gave_up_in_time(t0, gave_up, status)) return false;
   }
 }
 // The same for all warps of a block: one of them reads the counter, the others shared memory (2368 warps that read one line of
@@ -324,7 +331,8 @@ __device__ __forceinline__ void make_digits(const MoeParams& p, int row, unsigne
 
 // All items of a phase, by groups of ks warps.  J says what an item is: rows() its weights, scales() the factors of this lane's
 // two rows, columns() its digits, token() what the factor of a token is made of, finish() takes the sums of a token with these
-// rows (all lanes call it).  Behind the last item, `done` has gone up by the items of this call's warps.
+// rows (all lanes call it).  Behind the last item, `done` (if any) has gone up by the items of this call's
+// warps.
 //
 // Block b begins with the items b + blocks * group, and draws those behind them by tickets.  b is drawn too, so that blocks
 // that run have the first numbers; a group that finds no more tickets takes over the first items of a block that has not
@@ -474,7 +482,7 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
     if (cur >= items) break;
     if (gtid == 0) s_next[group] = items;
   }
-  if (part == 0) {
+  if (done != nullptr && part == 0) {
     __syncwarp();
     if (lane == 0 && finished) add_release(done, finished);
   }
@@ -612,19 +620,42 @@ struct Down {
     const int a = expert(item), c = 16 * (item - a * p.tiles) + u, row = ch.first[a] + r;
     const float f = digit_scale(top).factor, w = ch.prob[row];
     float* out = p.part + (size_t)row * p.C + c;
-    if (c < p.C) out[0] = __fmul_rn(w, __fmul_rn(__fmul_rn(low, f), s.x));
-    if (c + 8 < p.C) out[8] = __fmul_rn(w, __fmul_rn(__fmul_rn(high, f), s.y));
+    if (c < p.C) put(out, __fmul_rn(w, __fmul_rn(__fmul_rn(low, f), s.x)));
+    if (c + 8 < p.C) put(out + 8, __fmul_rn(w, __fmul_rn(__fmul_rn(high, f), s.y)));
   }
-  // The results of two tokens in a tile, by a warp.
+  static __device__ __forceinline__ void put(float* at, float v) {
+    const unsigned w = __float_as_uint(v);
+    asm volatile("st.relaxed.gpu.global.u32 [%0], %1;" ::"l"(at), "r"(w == kAbsent ? 0x7fffffffu : w) : "memory");
+  }
+  static __device__ __forceinline__ unsigned get(const float* at) {
+    unsigned w;
+    asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(w) : "l"(at) : "memory");
+    return w;
+  }
+  // The results of two tokens in a tile, by a warp.  The addends need no fence and no counter: a word is there or it is not.
   __device__ __forceinline__ void add_up(int t, int pair, int lane) const {
     const int c = 16 * t + (lane & 15);
-    if (c >= p.C) return;
     const int token = 2 * pair + (lane >> 4);
-    if (token >= p.T) return;
-    const int* rows = ch.row_of + token * p.k;
+    const bool live = c < p.C && token < p.T;
+    const int* rows = ch.row_of + (live ? token : 0) * p.k;
     float y = 0.0f;
-#pragma unroll 8
-    for (int j = 0; j < p.k; ++j) y = __fadd_rn(y, __ldcg(p.part + (size_t)rows[j] * p.C + c));
+    for (int j0 = 0; j0 < p.k; j0 += 8) {
+      unsigned w[8];
+      unsigned long long t0 = 0;
+      for (unsigned spins = 1;; ++spins) {
+        bool absent = false;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = live && j0 + j < p.k ? get(p.part + (size_t)rows[j0 + j] * p.C + c) : 0u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) absent |= w[j] == kAbsent;
+        if (!__any_sync(0xffffffffu, absent)) break;
+        if ((spins & 63u) == 0 && gave_up_in_time(t0, gave_up, p.status)) return;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j0 + j < p.k) y = __fadd_rn(y, __uint_as_float(w[j]));
+    }
+    if (!live) return;
     const long long at = (long long)token * p.ldy + c;
     if (p.x_type == Q8_F32) static_cast<float*>(p.y)[at] = y;
     else if (p.x_type == Q8_F16) static_cast<__half*>(p.y)[at] = __float2half_rn(y);
@@ -788,11 +819,10 @@ __global__ void __launch_bounds__(32 * warps_of(NT), 1) moe_experts_kernel(const
   }
   __syncthreads();
   const Down job{p, ch, largest, &p.sync[p.direct ? kDone1 : kDoneRows], (unsigned)(p.direct ? items1 : lay.rows), &s_known, &gave_up, own};
-  run_phase<NT, kGrid, kLater>(job, items2, (p.I + 63) >> 6, p.ks[1], &p.sync[kBlocks2], &p.sync[kDone2], s_block[1], s_next, acc, ring2, lane, warp);
+  run_phase<NT, kGrid, kLater>(job, items2, (p.I + 63) >> 6, p.ks[1], &p.sync[kBlocks2], static_cast<unsigned*>(nullptr), s_block[1], s_next, acc, ring2, lane, warp);
   // ---- the results, a warp sixteen channels of two tokens
   const int pairs = (p.T + 1) >> 1;
-  for (int u; (u = draw(&p.sync[kTiles])) < p.tiles * pairs;) {
-    if (!wait_counted(&p.sync[kDone2], (unsigned)items2, &gave_up, p.status)) break;
+  for (int u = (int)blockIdx.x + (int)gridDim.x * warp; u < p.tiles * pairs; u += (int)gridDim.x * kMoeWarps) {
     const int t = u / pairs;
     job.add_up(t, u - t * pairs, lane);
   }
