@@ -48,11 +48,10 @@ __host__ __device__ constexpr int depth2_of(int nt) { return (nt > 2 ? 48 : 64) 
 // Steps of digits in the hands of a warp with N columns, besides as many on their way.
 __host__ __device__ constexpr int ahead_of(int nt, int n) { return n == 2 && nt > 2 ? 4 : (n <= 4 ? 2 : 1); }
 constexpr float kDigitMax = 2139062016.0f;  // the largest fp32 number below 127 (256^3 + 256^2 + 256 + 1)
-// Tickets: blocks and items of phase one, of phase two, rows to be made digits; then how many items of phase one and rows are
-// done.  Each on a line of its own: who waits for one does not slow the others.
-enum { kLine = 32, kBlocks1 = 0, kItems1 = kLine, kBlocks2 = 2 * kLine, kItems2 = 3 * kLine, kRows = 4 * kLine, kDone1 = 5 * kLine, kDoneRows = 6 * kLine,
-       kCounters = 7 * kLine };
-constexpr unsigned kAbsent = 0xffffffffu;  // what stands in `part` until a result does (no operation gives this NaN)
+// Tickets: blocks and items of phase one, of phase two, rows to be made digits; then how many rows are.  Each on a line of its
+// own: who waits for one does not slow the others.
+enum { kLine = 32, kBlocks1 = 0, kItems1 = kLine, kBlocks2 = 2 * kLine, kItems2 = 3 * kLine, kRows = 4 * kLine, kDoneRows = 5 * kLine, kCounters = 6 * kLine };
+constexpr unsigned kAbsent = 0xffffffffu;  // what stands in `h` and `part` until a value does (no operation gives this NaN)
 constexpr int kDirectTokens = 4, kDirectSteps = 32; // tokens, and tokens times steps, up to which readers of inner activations make their digits themselves
 constexpr unsigned kTimeoutMoe = 32u;
 constexpr unsigned long long kMoeWaitNs = 2000000000ull;
@@ -78,14 +77,15 @@ struct MoeParams {
   // workspace
   double* logits;        // [T][E]
   float* x_factor;       // [T]
-  unsigned* sync;        // tickets and counters (kBlocks1 ..), then the largest magnitude of each row
+  unsigned* sync;        // tickets and counters (kBlocks1 ..)
+  unsigned* largest;     // largest magnitude of each row of inner activations
   float* part;           // weighted results of the experts [T k][C]
   signed char* xd;       // digits of the tokens [T][4][x_pitch]
   signed char* hd;       // digits of the inner activations [T k][4][h_pitch]
   float* h;              // inner activations [T k][h_pitch]
   int x_pitch, h_pitch;  // multiples of 128
   int unit_blocks, tiles, steps;  // items of an expert in phase one; items of phase two; steps of an item of phase one
-  int direct;                     // see kDirectSteps (until launch: the room it takes, or 0)
+  int direct;                     // see kDirectSteps: the room it takes in a warp's shared memory, or 0
   int ks[2];                      // warps that share the reduction of an item, by phase
   Divide by_unit_blocks, by_tiles;
   int x_vec, r_vec;
@@ -147,14 +147,15 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  {
-    uint4* part = reinterpret_cast<uint4*>(p.part);
-    const size_t n = ((size_t)p.T * p.k * p.C + 3) / 4;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) part[i] = make_uint4(kAbsent, kAbsent, kAbsent, kAbsent);
-  }
+  auto clear = [&](float* at, size_t n) {
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < (n + 3) / 4; i += (size_t)gridDim.x * 256)
+      reinterpret_cast<uint4*>(at)[i] = make_uint4(kAbsent, kAbsent, kAbsent, kAbsent);
+  };
+  clear(p.part, (size_t)p.T * p.k * p.C);
+  clear(p.h, (size_t)p.T * p.k * p.h_pitch);
   if ((int)blockIdx.x < p.T) {  // digits of a token
     const int t = blockIdx.x;
-    if (t == 0) for (int i = threadIdx.x; i < kCounters + p.T * p.k; i += 256) p.sync[i] = 0u;
+    if (t == 0) for (int i = threadIdx.x; i < kCounters; i += 256) p.sync[i] = 0u;
     __shared__ unsigned part[8];
     unsigned m = 0;
     if (p.x_vec) {
@@ -256,7 +257,7 @@ struct MoeChoice {
   float* prob;          // [rows] by row
   int* row_of;          // [T][k] rows of a token, ascending
   int* row_token;       // [rows]
-  int* row_at;          // [rows] place of the row's expert among the chosen
+  unsigned* top;        // [rows] largest magnitude of its inner activations, kAbsent until it is known (direct alone)
 };
 
 __device__ __forceinline__ unsigned load_acquire(const unsigned* p) {
@@ -308,37 +309,73 @@ __device__ __forceinline__ void wait_block(const unsigned* counter, unsigned n, 
 }
 
 
-__device__ __forceinline__ float4 load_h4(const MoeParams& p, int row, int i) {
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (i < p.I) v = __ldcg(reinterpret_cast<const float4*>(p.h + (size_t)row * p.h_pitch + i));
-  if (i + 1 >= p.I) v.y = 0.0f;
-  if (i + 2 >= p.I) v.z = 0.0f;
-  if (i + 3 >= p.I) v.w = 0.0f;
+// Words that are values, or not there yet: they need neither fences nor counters.
+__device__ __forceinline__ void put_word(float* at, float v) {
+  const unsigned w = __float_as_uint(v);
+  asm volatile("st.relaxed.gpu.global.u32 [%0], %1;" ::"l"(at), "r"(w == kAbsent ? 0x7fffffffu : w) : "memory");
+}
+__device__ __forceinline__ unsigned get_word(const float* at) {
+  unsigned w;
+  asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(w) : "l"(at) : "memory");
+  return w;
+}
+
+// Four inner activations from i on, zero behind the row's end.
+__device__ __forceinline__ uint4 load_h4(const MoeParams& p, int row, int i) {
+  uint4 v = make_uint4(0u, 0u, 0u, 0u);
+  if (i < p.I) {
+    const float* at = p.h + (size_t)row * p.h_pitch + i;
+    asm volatile("ld.relaxed.gpu.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(at) : "memory");
+  }
+  if (i + 1 >= p.I) v.y = 0u;
+  if (i + 2 >= p.I) v.z = 0u;
+  if (i + 3 >= p.I) v.w = 0u;
   return v;
 }
-// The digits of one row of inner activations, by a warp; zero behind the row's end.
-__device__ __forceinline__ void make_digits(const MoeParams& p, int row, unsigned largest, int lane) {
-  const DigitScale s = digit_scale(largest);
-  signed char* out = p.hd + (size_t)row * 4 * p.h_pitch;
-#pragma unroll 8
-  for (int i = 4 * lane; i < p.h_pitch; i += 128) {
-    unsigned d[4];
-    digits_4(load_h4(p, row, i), s, d);
+// The largest magnitude of a row of inner activations once all of them are there (or time is up), by a warp.
+__device__ __forceinline__ unsigned row_top(const MoeParams& p, int row, int lane, int* gave_up) {
+  unsigned m = 0;
+  unsigned long long t0 = 0;
+  for (int i = 4 * lane; i - 4 * lane < p.I; i += 512) {
+    for (unsigned spins = 1;; ++spins) {
+      uint4 v[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) *reinterpret_cast<unsigned*>(out + j * (size_t)p.h_pitch + i) = d[j];
+      for (int j = 0; j < 4; ++j) v[j] = load_h4(p, row, i + 128 * j);
+      bool absent = false;
+      unsigned top = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        absent |= v[j].x == kAbsent || v[j].y == kAbsent || v[j].z == kAbsent || v[j].w == kAbsent;
+        top = max(max(top, max(v[j].x & 0x7fffffffu, v[j].y & 0x7fffffffu)), max(v[j].z & 0x7fffffffu, v[j].w & 0x7fffffffu));
+      }
+      if (!__any_sync(0xffffffffu, absent)) { m = max(m, top); break; }
+      if ((spins & 63u) == 0 && gave_up_in_time(t0, gave_up, p.status)) return 0x7fffffffu;
+    }
+  }
+  return warp_max(m);
+}
+// The digits of inner activations of a row from i0 on, by a warp; zero behind the row's end.
+__device__ __forceinline__ void make_digits(const MoeParams& p, int row, unsigned top, int i0, int len, signed char* out, int pitch, int lane) {
+  const DigitScale s = digit_scale(top);
+#pragma unroll 8
+  for (int i = 4 * lane; i < len; i += 128) {
+    const uint4 v = load_h4(p, row, i0 + i);
+    unsigned d[4];
+    digits_4(make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)), s, d);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<unsigned*>(out + j * (size_t)pitch + i) = d[j];
   }
 }
 
 // All items of a phase, by groups of ks warps.  J says what an item is: rows() its weights, scales() the factors of this lane's
 // two rows, columns() its digits, token() what the factor of a token is made of, finish() takes the sums of a token with these
-// rows (all lanes call it).  Behind the last item, `done` (if any) has gone up by the items of this call's
-// warps.
+// rows (all lanes call it).
 //
 // Block b begins with the items b + blocks * group, and draws those behind them by tickets.  b is drawn too, so that blocks
 // that run have the first numbers; a group that finds no more tickets takes over the first items of a block that has not
 // drawn its number.  Whoever then waits for an item knows it in the hands of a running warp.
 template <int NT, int kGrid, int kDepth, typename J>
-__device__ __forceinline__ void run_phase(const J& job, int items, int steps, int ks, unsigned* tickets, unsigned* done, int block, int* s_next, int* acc_all,
+__device__ __forceinline__ void run_phase(const J& job, int items, int steps, int ks, unsigned* tickets, int block, int* s_next, int* acc_all,
                                           const unsigned char* ring_at, int lane, int warp) {
   const int group = warp / ks, part = warp - group * ks, gtid = part * 32 + lane, threads = 32 * ks, i = lane & 3, g = lane >> 2;
   const int per = (steps + ks - 1) / ks, s0 = min(steps, part * per), n = min(steps, s0 + per) - s0;
@@ -360,7 +397,6 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
   }
   Ring<kGrid, kDepth> ring;
   ring.init(ring_at, lane);
-  unsigned finished = 0;
   const int slots = max(n, kDepth);  // of an item: with fewer steps than the ring has slots, some stay empty
   for (;;) {
     Rows r = job.rows(cur, items, s0, n, lane);
@@ -461,7 +497,6 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
       else if (count <= 8) go(std::integral_constant<int, (NT < 4 ? NT : 4)>{});
       else go(std::integral_constant<int, NT>{});
       if (n == 0 && nxt < items) r = next;
-      ++finished;
       cur = nxt;
     }
     if (gtid == 0) {
@@ -481,10 +516,6 @@ __device__ __forceinline__ void run_phase(const J& job, int items, int steps, in
     meet();
     if (cur >= items) break;
     if (gtid == 0) s_next[group] = items;
-  }
-  if (done != nullptr && part == 0) {
-    __syncwarp();
-    if (lane == 0 && finished) add_release(done, finished);
   }
 }
 
@@ -514,7 +545,6 @@ struct MoeShared {
 struct GateUp {
   const MoeParams& p;
   const MoeChoice& ch;
-  unsigned* largest;
   const signed char* digits;  // of the tokens, in shared memory or not
   int pitch;
   __device__ __forceinline__ int expert(int item) const { return p.by_unit_blocks(item); }
@@ -544,19 +574,12 @@ struct GateUp {
   __device__ __forceinline__ unsigned token(int item, int r) const { return __float_as_uint(__ldg(p.x_factor + ch.row_token[ch.first[expert(item)] + r])); }
   __device__ __forceinline__ void finish(int item, int r, int u, bool live, float gate, float up, float2 s, unsigned factor) const {
     const int a = expert(item), i = (item - a * p.unit_blocks) * 8 + u, row = ch.first[a] + r;
-    unsigned m = 0;
     if (live && i < p.I) {
       const float f = __uint_as_float(factor);
       const float g = __fmul_rn(__fmul_rn(gate, f), s.x), v = __fmul_rn(__fmul_rn(up, f), s.y);
       const float h = __fmul_rn(__fdividef(g, __fadd_rn(1.0f, expf(-g))), v);  // (divided within 2 ulp, or 0 for gates below -87)
-      p.h[(size_t)row * p.h_pitch + i] = h;
-      m = abs_word(h);
+      put_word(p.h + (size_t)row * p.h_pitch + i, h);
     }
-    // the eight units of a token are eight lanes four apart
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 4));
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 8));
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 16));
-    if (live && u == 0) atomicMax(&largest[row], m);
   }
 };
 
@@ -564,11 +587,20 @@ struct GateUp {
 struct Down {
   const MoeParams& p;
   const MoeChoice& ch;
-  const unsigned* largest;
-  const unsigned* waited;  // a counter and what it has to reach before digits are read
-  unsigned reached;
   int *known, *gave_up;    // (shared memory) see wait_block
-  signed char* mine;  // shared memory of this warp for an item's digits
+  signed char* mine;       // shared memory of this warp for an item's digits
+  int warp, warps;
+  mutable bool looked;
+  // The warps of a block share the rows whose largest magnitudes it needs.  (Called with the first weights on their way.)
+  __device__ __forceinline__ void look(int lane) const {
+    if (looked || !p.direct) return;
+    looked = true;
+    for (int r = warp; r < p.T * p.k; r += warps) {
+      const unsigned top = row_top(p, r, lane, gave_up);
+      __threadfence_block();
+      if (lane == 0) *const_cast<volatile unsigned*>(ch.top + r) = top;
+    }
+  }
   __device__ __forceinline__ int expert(int item) const { return p.by_tiles(item); }
   __device__ __forceinline__ int count(int item) const { return __popc(ch.tokens[expert(item)]); }
   __device__ __forceinline__ Rows rows(int item, int items, int s0, int n, int lane) const {
@@ -584,26 +616,22 @@ struct Down {
   template <int NT>
   __device__ __forceinline__ void columns(int item, int count, int s0, int n, int lane, const signed char* (&z)[NT]) const {
     const int a = expert(item), first = ch.first[a], digit = (lane >> 2) & 3;
-    wait_block(waited, reached, known, gave_up, p.status);
     if (!p.direct) {
+      wait_block(&p.sync[kDoneRows], (unsigned)(p.T * p.k), known, gave_up, p.status);
       const signed char* from = p.hd + (size_t)first * 4 * p.h_pitch + 64 * s0 + 16 * (lane & 3);
 #pragma unroll
       for (int t = 0; t < NT; ++t) z[t] = from + (size_t)(min(2 * t + (lane >> 4), count - 1) * 4 + digit) * p.h_pitch;
       return;
     }
     // digits made here, in the warp's own shared memory
-    const int pitch = staged_pitch(n), len = 64 * n;
+    const int pitch = staged_pitch(n);
     __syncwarp();  // (all lanes have read what was there)
-    const unsigned top = lane < count ? __ldcg(largest + first + lane) : 0u;
+    look(lane);
     for (int r = 0; r < count; ++r) {
-      const DigitScale scale = digit_scale(__shfl_sync(0xffffffffu, top, r));
-#pragma unroll 8
-      for (int c = 4 * lane; c < len; c += 128) {
-        unsigned d[4];
-        digits_4(load_h4(p, first + r, 64 * s0 + c), scale, d);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) *reinterpret_cast<unsigned*>(mine + (4 * r + j) * pitch + c) = d[j];
-      }
+      unsigned top;
+      while (!__all_sync(0xffffffffu, (top = *const_cast<volatile unsigned*>(ch.top + first + r)) != kAbsent)) __nanosleep(20);  // (who looks stops in time)
+      __threadfence_block();
+      make_digits(p, first + r, top, 64 * s0, 64 * n, mine + 4 * r * pitch, pitch, lane);
     }
     __syncwarp();
 #pragma unroll
@@ -614,25 +642,16 @@ struct Down {
     const float* s = p.sd + (size_t)ch.expert[a] * p.C;
     return make_float2(__ldg(s + min(c, p.C - 1)), __ldg(s + min(c + 8, p.C - 1)));
   }
-  __device__ __forceinline__ unsigned token(int item, int r) const { return __ldcg(largest + ch.first[expert(item)] + r); }
+  __device__ __forceinline__ unsigned token(int item, int r) const { const int row = ch.first[expert(item)] + r; return p.direct ? ch.top[row] : __ldcg(p.largest + row); }
   __device__ __forceinline__ void finish(int item, int r, int u, bool live, float low, float high, float2 s, unsigned top) const {
     if (!live) return;
     const int a = expert(item), c = 16 * (item - a * p.tiles) + u, row = ch.first[a] + r;
     const float f = digit_scale(top).factor, w = ch.prob[row];
     float* out = p.part + (size_t)row * p.C + c;
-    if (c < p.C) put(out, __fmul_rn(w, __fmul_rn(__fmul_rn(low, f), s.x)));
-    if (c + 8 < p.C) put(out + 8, __fmul_rn(w, __fmul_rn(__fmul_rn(high, f), s.y)));
+    if (c < p.C) put_word(out, __fmul_rn(w, __fmul_rn(__fmul_rn(low, f), s.x)));
+    if (c + 8 < p.C) put_word(out + 8, __fmul_rn(w, __fmul_rn(__fmul_rn(high, f), s.y)));
   }
-  static __device__ __forceinline__ void put(float* at, float v) {
-    const unsigned w = __float_as_uint(v);
-    asm volatile("st.relaxed.gpu.global.u32 [%0], %1;" ::"l"(at), "r"(w == kAbsent ? 0x7fffffffu : w) : "memory");
-  }
-  static __device__ __forceinline__ unsigned get(const float* at) {
-    unsigned w;
-    asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(w) : "l"(at) : "memory");
-    return w;
-  }
-  // The results of two tokens in a tile, by a warp.  The addends need no fence and no counter: a word is there or it is not.
+  // The results of two tokens in a tile once their addends are there, by a warp.
   __device__ __forceinline__ void add_up(int t, int pair, int lane) const {
     const int c = 16 * t + (lane & 15);
     const int token = 2 * pair + (lane >> 4);
@@ -645,7 +664,7 @@ struct Down {
       for (unsigned spins = 1;; ++spins) {
         bool absent = false;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = live && j0 + j < p.k ? get(p.part + (size_t)rows[j0 + j] * p.C + c) : 0u;
+        for (int j = 0; j < 8; ++j) w[j] = live && j0 + j < p.k ? get_word(p.part + (size_t)rows[j0 + j] * p.C + c) : 0u;
 #pragma unroll
         for (int j = 0; j < 8; ++j) absent |= w[j] == kAbsent;
         if (!__any_sync(0xffffffffu, absent)) break;
@@ -677,8 +696,8 @@ __global__ void __launch_bounds__(32 * warps_of(NT), 1) moe_experts_kernel(const
   ch.first = reinterpret_cast<int*>(ch.tokens + lay.rows);
   ch.prob = reinterpret_cast<float*>(ch.first + lay.rows);
   ch.row_of = reinterpret_cast<int*>(ch.prob + lay.rows);
-  ch.row_at = ch.row_of + lay.rows;
-  ch.row_token = ch.row_at + lay.rows;
+  ch.top = reinterpret_cast<unsigned*>(ch.row_of + lay.rows);
+  ch.row_token = reinterpret_cast<int*>(ch.top + lay.rows);
   unsigned* const mask = reinterpret_cast<unsigned*>(ch.row_token + lay.rows);  // [E] tokens that chose an expert
   int* const index = reinterpret_cast<int*>(mask + p.E);                          // [E] its place among the chosen
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -789,19 +808,18 @@ __global__ void __launch_bounds__(32 * warps_of(NT), 1) moe_experts_kernel(const
       for (int j = 0; j < p.k; ++j) place += __shfl_sync(p.k == 32 ? 0xffffffffu : (1u << p.k) - 1u, mine[w], j) < mine[w];
       ch.prob[row] = weight[w];
       ch.row_of[t * p.k + place] = row;
-      ch.row_at[row] = at;
+      ch.top[row] = kAbsent;
       ch.row_token[row] = t;
     }
   }
   const int active = s_active;
-  unsigned* const largest = p.sync + kCounters;
 
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
   const int items1 = active * p.unit_blocks, items2 = active * p.tiles;
   {
-    const GateUp job{p, ch, largest, lay.staged ? digits : p.xd, lay.staged ? x_staged : p.x_pitch};
-    run_phase<NT, kGrid, depth1_of(NT)>(job, items1, p.steps, p.ks[0], &p.sync[kBlocks1], &p.sync[kDone1], s_block[0], s_next, acc, ring1, lane, warp);
+    const GateUp job{p, ch, lay.staged ? digits : p.xd, lay.staged ? x_staged : p.x_pitch};
+    run_phase<NT, kGrid, depth1_of(NT)>(job, items1, p.steps, p.ks[0], &p.sync[kBlocks1], s_block[0], s_next, acc, ring1, lane, warp);
   }
   auto draw = [&](unsigned* ticket) {
     int v = 0;
@@ -811,15 +829,17 @@ __global__ void __launch_bounds__(32 * warps_of(NT), 1) moe_experts_kernel(const
   // ---- the rows of inner activations become digits, a warp a row
   if (!p.direct) {
     for (int row; (row = draw(&p.sync[kRows])) < lay.rows;) {
-      if (!wait_counted(&p.sync[kDone1], (unsigned)items1, &gave_up, p.status)) break;
-      make_digits(p, row, __ldcg(largest + row), lane);
+      const unsigned top = row_top(p, row, lane, &gave_up);
+      if (lane == 0) p.largest[row] = top;
+      make_digits(p, row, top, 0, p.h_pitch, p.hd + (size_t)row * 4 * p.h_pitch, p.h_pitch, lane);
       __syncwarp();
       if (lane == 0) add_release(&p.sync[kDoneRows], 1u);
     }
   }
   __syncthreads();
-  const Down job{p, ch, largest, &p.sync[p.direct ? kDone1 : kDoneRows], (unsigned)(p.direct ? items1 : lay.rows), &s_known, &gave_up, own};
-  run_phase<NT, kGrid, kLater>(job, items2, (p.I + 63) >> 6, p.ks[1], &p.sync[kBlocks2], static_cast<unsigned*>(nullptr), s_block[1], s_next, acc, ring2, lane, warp);
+  const Down job{p, ch, &s_known, &gave_up, own, warp, kMoeWarps, false};
+  run_phase<NT, kGrid, kLater>(job, items2, (p.I + 63) >> 6, p.ks[1], &p.sync[kBlocks2], s_block[1], s_next, acc, ring2, lane, warp);
+  job.look(lane);  // (of a warp without an item)
   // ---- the results, a warp sixteen channels of two tokens
   const int pairs = (p.T + 1) >> 1;
   for (int u = (int)blockIdx.x + (int)gridDim.x * warp; u < p.tiles * pairs; u += (int)gridDim.x * kMoeWarps) {
@@ -864,7 +884,8 @@ size_t moe_space(const q8_moe_desc& d, char* ws, MoeParams* p) {
   auto take = [&](size_t bytes) { char* q = ws + at; at += up256(bytes); return q; };
   p->logits = reinterpret_cast<double*>(take(T * d.E * sizeof(double)));
   p->x_factor = reinterpret_cast<float*>(take(T * 4));
-  p->sync = reinterpret_cast<unsigned*>(take((kCounters + rows) * 4));
+  p->sync = reinterpret_cast<unsigned*>(take(kCounters * 4));
+  p->largest = reinterpret_cast<unsigned*>(take(rows * 4));
   p->xd = reinterpret_cast<signed char*>(take(T * 4 * pitch128(d.C) + kOverread));
   p->hd = reinterpret_cast<signed char*>(take(rows * 4 * pitch128(d.I) + kOverread));
   p->part = reinterpret_cast<float*>(take(rows * d.C * 4));
@@ -887,7 +908,7 @@ template <int NT, int kGrid>
 int launch_experts(MoeParams p, cudaStream_t s) {
   const MoeShared lay(p.T, p.k, p.E, p.steps, Ring<kGrid, 1>::kStep, NT);
   const int smem = lay.total;
-  p.direct = p.direct != 0 && p.direct <= lay.room;
+  if (p.direct > lay.room) p.direct = 0;
   static std::atomic<bool> set[kMaxDevices];
   const int dev = current_device();
   if (dev < 0 || !set[dev].load(std::memory_order_relaxed)) {
