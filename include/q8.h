@@ -400,8 +400,8 @@ int q8_detection_output(int n_sources, const float* const* loc, const int* loc_s
  * Token operators (the paper has no counterpart): the 8-bit products of language models, whose activations have no
  * calibrated factor.  A tensor of activations is a matrix of tokens (rows) by channels with a row pitch in elements
  * (ldx >= C: a slice of a wider tensor will do); each token carries a factor of its own, found from its values when
- * it is quantized, and each output channel of a weight matrix [K][C] its own, max|w[k]| / 127 (q8_calibrate_maxabs_rows,
- * q8_factor, q8_quantize_rows).
+ * it is quantized, and each output channel of a weight matrix [K][C] its own, max|w[k]| / 127 (q8_quantize_tokens of its rows
+ * gives codes and factors).
  * ---------------------------------------------------------------------- */
 
 /* Codes and factors of `tokens` rows of C values of x_type (Q8_F32, Q8_F16 or Q8_BF16, converted to fp32 exactly):
@@ -434,7 +434,8 @@ typedef struct q8_linear_desc {
 } q8_linear_desc;
 
 /* Bytes of device scratch with which q8_linear runs `d` fastest, given 16-byte aligned pointers (0 for many): the codes
- * and factors of floating-point activations, and copies on the 16-byte grid of codes and weights off it.  Host only. */
+ * and factors of floating-point activations, and copies on the 16-byte grid of codes and weights off it (for a pointer off
+ * the grid, ask with a pitch off it).  Host only. */
 int q8_linear_workspace_bytes(const q8_linear_desc* d, size_t* bytes);
 
 /* x: device [M][ldx] (x_type).  x_scale: device fp32 [M] or NULL (see above).  w: device s8 [K][ldw].  w_scale: device fp32
@@ -454,8 +455,9 @@ int q8_linear(const q8_linear_desc* d, const void* x, const float* x_scale, cons
  *   g = (x . w_gate_up[e][i]) * s_gate_up[e][i],  u = (x . w_gate_up[e][I + i]) * s_gate_up[e][I + i],  i < I
  *   h[i] = g / (1 + exp(-g)) * u
  *   y[t][c] = sum over the chosen e of p * ((h . w_down[e][c]) * s_down[e][c])
- * Activations and h are not rounded to 8 bits: they keep 24 bits or more, of the largest of their row or of their own, and results are
- * those of 32-bit arithmetic.  The same inputs give the same bits whatever the other tokens of the call are. */
+ * Activations and h are not rounded to 8 bits: they are held to 3 * 2^-24 of themselves and 2^-31 of the largest of their row,
+ * and sums over them are exact, so results are those of 32-bit arithmetic.  The same inputs give the same bits whatever the other
+ * tokens of the call are. */
 typedef struct q8_moe_desc {
   int64_t ldx, ldy;         /* elements from one token to the next; 0: C */
   int32_t T, C, I, E;       /* tokens, width, inner width of an expert, experts */
@@ -472,8 +474,8 @@ int q8_moe_workspace_bytes(const q8_moe_desc* d, size_t* bytes);
  * rows; s_gate_up: device fp32 [E][2 I].  w_down: device s8 [E][C][I]; s_down: device fp32 [E][C].  y: device [T][ldy], of
  * which the C values of a row are written; may not overlap an input.  ids: device s32 [T][top_k] or NULL, the chosen experts;
  * probs: device fp32 [T][top_k] or NULL, their p.  workspace: device, 256-byte aligned; contents undefined before and after;
- * calls that may overlap on the GPU need one each.  T == 0 is allowed.  Any T runs, tokens in groups of 16, each of which
- * reads the weights of its experts: meant for few tokens.  Weights whose rows lie on the 16-byte grid (C and I multiples
+ * calls that may overlap on the GPU need one each.  T == 0 is allowed.  Any T runs, tokens in groups of 16 (256 / top_k
+ * where that is less), each of which reads the weights of its experts: meant for few tokens.  Weights whose rows lie on the 16-byte grid (C and I multiples
  * of 16, pointers aligned) are faster.
  * Limits: C, I <= 131071, E <= 1024, top_k <= min(E, 32).
  * Errors: Q8_ERR_INVALID_ARG (null pointer, extents, pitches, types), Q8_ERR_UNSUPPORTED (a limit), Q8_ERR_ALIGNMENT (a

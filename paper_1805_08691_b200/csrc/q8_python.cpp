@@ -508,7 +508,10 @@ PyObject* py_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const q8_linear_desc d{x.ld, w.ld, y.ld, (int32_t)x.rows, (int32_t)x.C, (int32_t)K, x.type, y.type, 0};
   size_t need = 0, bytes = 0;
   at::Tensor own;
-  int rc = a[7] == Py_None ? g_q8.linear_bytes(&d, &need) : Q8_OK;
+  q8_linear_desc asked = d;  // rows that begin off the 16-byte grid need what those with a pitch off it do
+  if (reinterpret_cast<uintptr_t>(x.p) % 16) asked.ldx |= 1;
+  if (reinterpret_cast<uintptr_t>(w.p) % 16) asked.ldw |= 1;
+  int rc = a[7] == Py_None ? g_q8.linear_bytes(&asked, &need) : Q8_OK;
   if (rc == Q8_OK) {
     if (!workspace_of(a[7], need, *x.t, &own, &space, &bytes)) return nullptr;
     void* stream = current_stream();
