@@ -45,7 +45,7 @@ def _native_command(out):
             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + os.path.join(ROOT, "include"),
             *(w for d in system if d for w in ("-isystem", d)),
             os.path.join(CSRC, "q8_python.cpp"), "-o", out, "-L" + os.path.join(t, "lib"),
-            "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+            "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"]
 
 
 def _older(path, deps) -> bool:

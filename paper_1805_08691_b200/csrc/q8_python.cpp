@@ -8,7 +8,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
-#include <ATen/ops/empty.h>
+#include <ATen/cuda/EmptyTensor.h>
 
 #include <cstdint>
 #include <vector>
@@ -389,14 +389,19 @@ bool dense(PyObject* o, const char* what, at::IntArrayRef shape, at::ScalarType 
   return values(o, what, t->numel(), st, st_name, false, p);
 }
 
-// The tensor given, or a new one like those of `like` with sizes[..., last].
+// A new tensor where `like` is, past the dispatcher (a fifth of the time of at::empty less, which an eager call of a small kernel
+// feels: codes and factors of one token 5.1 -> 4.8 us on the host).
+at::Tensor fresh(at::IntArrayRef sizes, const at::Tensor& like, at::ScalarType st) {
+  return at::Tensor(at::detail::empty_cuda(sizes, st, like.device(), std::nullopt));
+}
+// ... with the sizes of `like` but for the last, and without it.
 at::Tensor made(const at::Tensor& like, int64_t last, at::ScalarType st) {
   auto sizes = like.sizes().vec();
   sizes.back() = last;
-  return at::empty(sizes, like.options().dtype(st).requires_grad(false));
+  return fresh(sizes, like, st);
 }
 at::Tensor made_scalar_per_row(const at::Tensor& like, at::ScalarType st) {
-  return at::empty(like.sizes().slice(0, like.dim() - 1), like.options().dtype(st).requires_grad(false));
+  return fresh(like.sizes().slice(0, like.dim() - 1), like, st);
 }
 
 // The interpreter's status for a call that has written `result` (stolen): (status, result).
@@ -472,7 +477,7 @@ bool workspace_of(PyObject* o, size_t need, const at::Tensor& like, at::Tensor* 
     *p = nullptr;
     *bytes = need;
     if (need) {
-      *own = at::empty({(int64_t)need}, like.options().dtype(at::kByte).requires_grad(false));
+      *own = fresh({(int64_t)need}, like, at::kByte);
       *p = own->data_ptr();
     }
     return true;
