@@ -3,12 +3,13 @@
 // Bound by memory.  A team of threads (a warp, or a block of 128, 256 or 512) takes a token and holds its values in registers
 // between the maximum and the codes, so that they are read from memory once; what a team cannot hold is read a second time,
 // from L2.  Teams are as large as leaves a thread about four pieces of 16 bytes (64 bytes in flight each), and with fewer tokens
-// than that occupies the GPU large enough for one each: one token of 4096 values is then 1.6 us of latency and nothing else.
-// Registers are held to what five blocks of 256 threads leave (8192 x 4096 f32: 33 us, with 512 threads a row 45).
+// than that occupies the GPU large enough for one each: one token of 4096 values is then 1.5 us of latency and nothing else.
+// Registers are held to what five blocks of 256 threads leave (8192 x 4096 f32: 31 us, with 512 threads a row 45).
 // Rows off the 16-byte grid: four 16-bit values that adjoin, or four fp32 values as far apart as the team is large, so that a
-// warp's addresses adjoin (1000 x 2051 f32: 5.0 us against 5.6; 8192 x 2678 f16: 31 us against 34 the other way round), and so
+// warp's addresses adjoin (1000 x 2051 f32: 5.0 us against 5.6; 8192 x 2678 f16: 32 us against 34 the other way round), and so
 // on the way back for all types (8192 x 2678 f16: 21 us against 26).
-// 8192 x 4096 bf16: 22 us to codes (4.6 TB/s of 6.5 measured), 19 us back (5.3 TB/s); the first form here, a block a token that
+// 8192 x 4096 bf16: 21 us to codes (4.7 TB/s of 6.5 measured; half of the rest is instructions: a scheduler issues in 70 % of
+// its cycles), 19 us back (5.2 TB/s); the first form here, a block a token that
 // read its row twice, value by value, 73 us for both.
 #include "q8_token_common.cuh"
 
@@ -17,23 +18,24 @@ namespace {
 
 constexpr int kHeld = 4;  // chunks a thread holds
 
-// Sixteen bytes of a row (V values), or four values; those from C on are zero.
+// Sixteen bytes of a row (V values), or four values: from `at` on, where `left` values of the row remain; those
+// behind them are zero.
 template <typename T, bool kVec, int kTeam>
 struct Chunk {
   static constexpr int V = kVec ? 16 / (int)sizeof(T) : 4;
   static constexpr int kStep = kVec || sizeof(T) == 2 ? 1 : kTeam;  // from value to value
   unsigned w[V * sizeof(T) / 4];
-  __device__ __forceinline__ void load(const T* row, size_t c, size_t C) {
-    if (kVec && c + V <= C) {
-      *reinterpret_cast<uint4*>(w) = __ldg(reinterpret_cast<const uint4*>(row + c));
+  __device__ __forceinline__ void load(const T* at, int left) {
+    if (kVec && V <= left) {
+      *reinterpret_cast<uint4*>(w) = __ldg(reinterpret_cast<const uint4*>(at));
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const bool live = c + j * kStep < C;
+        const bool live = j * kStep < left;
         if constexpr (sizeof(T) == 4) {
-          w[j] = live ? reinterpret_cast<const unsigned*>(row)[c + j * kStep] : 0u;
+          w[j] = live ? reinterpret_cast<const unsigned*>(at)[j * kStep] : 0u;
         } else {
-          const unsigned h = live ? reinterpret_cast<const unsigned short*>(row)[c + j * kStep] : 0u;
+          const unsigned h = live ? reinterpret_cast<const unsigned short*>(at)[j * kStep] : 0u;
           w[j / 2] = j & 1 ? w[j / 2] | h << 16 : h;
         }
       }
@@ -47,8 +49,8 @@ struct Chunk {
       else m = max_two(m, w[j]);
     }
   }
-  // z: the row's codes
-  __device__ __forceinline__ void store(signed char* z, size_t c, size_t C, const TokenFactor& f) const {
+  // z: the codes' place
+  __device__ __forceinline__ void store(signed char* z, int left, const TokenFactor& f) const {
     unsigned o[V / 4];
 #pragma unroll
     for (int j = 0; j < V / 4; ++j) {
@@ -62,13 +64,13 @@ struct Chunk {
       }
       o[j] = f.finite ? codes_4(v, f) : 0u;
     }
-    if (kVec && c + V <= C) {
-      if constexpr (V == 8) *reinterpret_cast<uint2*>(z + c) = make_uint2(o[0], o[1]);
-      else *reinterpret_cast<unsigned*>(z + c) = o[0];
+    if (kVec && V <= left) {
+      if constexpr (V == 8) *reinterpret_cast<uint2*>(z) = make_uint2(o[0], o[1]);
+      else *reinterpret_cast<unsigned*>(z) = o[0];
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j)
-        if (c + j * kStep < C) z[c + j * kStep] = (signed char)(o[j / 4] >> (8 * (j & 3)));
+        if (j * kStep < left) z[j * kStep] = (signed char)(o[j / 4] >> (8 * (j & 3)));
     }
   }
 };
@@ -85,7 +87,7 @@ __device__ __forceinline__ unsigned as_fp32_bits(unsigned m) {  // of a maximum 
 
 // Teams of kTeam threads, a token each.  kTeam 32: eight tokens a block.
 template <typename T, bool kVec, int kTeam>
-__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? (sizeof(T) == 4 ? 3 : 2) : (kTeam == 128 ? 10 : 5)) quantize_tokens_kernel(const T* __restrict__ x, size_t tokens, size_t C, size_t ldx,
+__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : (kTeam == 128 ? 10 : 5)) quantize_tokens_kernel(const T* __restrict__ x, size_t tokens, size_t C, size_t ldx,
                                                                                     signed char* __restrict__ z, size_t ldz, float* __restrict__ scale) {
   using Part = Chunk<T, kVec, kTeam>;
   __shared__ unsigned part[kTeam / 32];
@@ -98,17 +100,21 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? (siz
   signed char* out = z + t * ldz;
   constexpr int kTurn = kTeam * Part::V;
   const size_t c0 = (size_t)tid * (Part::kStep == 1 ? Part::V : 1);
+  if (C <= c0) C = c0;
+  const int left = (int)min(C - c0, (size_t)1 << 30);  // (more than is held)
+  row += c0;
+  out += c0;
   Part held[kHeld];
   unsigned m = 0;
 #pragma unroll
   for (int j = 0; j < kHeld; ++j)
-    if (c0 + j * kTurn < C) held[j].load(row, c0 + j * kTurn, C);
+    if (j * kTurn < left) held[j].load(row + j * kTurn, left - j * kTurn);
 #pragma unroll
   for (int j = 0; j < kHeld; ++j)
-    if (c0 + j * kTurn < C) held[j].max_into(m);
-  for (size_t c = c0 + kHeld * kTurn; c < C; c += kTurn) {
+    if (j * kTurn < left) held[j].max_into(m);
+  for (size_t c = kHeld * kTurn; c < C - c0; c += kTurn) {
     Part again;
-    again.load(row, c, C);
+    again.load(row + c, (int)min(C - c0 - c, (size_t)1 << 30));
     again.max_into(m);
   }
   m = warp_max(as_fp32_bits<T>(m));
@@ -122,11 +128,11 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? (siz
   if (tid == 0) scale[t] = f.s;
 #pragma unroll
   for (int j = 0; j < kHeld; ++j)
-    if (c0 + j * kTurn < C) held[j].store(out, c0 + j * kTurn, C, f);
-  for (size_t c = c0 + kHeld * kTurn; c < C; c += kTurn) {
+    if (j * kTurn < left) held[j].store(out + j * kTurn, left - j * kTurn, f);
+  for (size_t c = kHeld * kTurn; c < C - c0; c += kTurn) {
     Part again;
-    again.load(row, c, C);
-    again.store(out, c, C, f);
+    again.load(row + c, (int)min(C - c0 - c, (size_t)1 << 30));
+    again.store(out + c, (int)min(C - c0 - c, (size_t)1 << 30), f);
   }
 }
 
