@@ -1,4 +1,4 @@
-// The product with a factor per token for few tokens, and for operands off the 16-byte grid.
+// The product with a factor per token without scratch, for any operands.
 //
 //   D[16 output channels, 8 NT tokens] (int32, registers) = W[16, C] (from global memory) x Z[8 NT, C]^T (shared memory)
 //
@@ -7,6 +7,9 @@
 // weight row are its operands of two instructions as they come, without shared memory or shuffles, and 16 bytes of a token's
 // codes are the other operand.  The partial sums of the warps meet in shared memory (integers: any order, same result).
 // Floating-point activations become codes while they are staged.
+//
+// It is there for calls without scratch, whose activations every block quantizes for itself: 64 tokens of bf16, 4096 -> 4096
+// 195 us (8.6 with scratch); 300 tokens of codes off the grid, 1001 -> 130 12.9 us (8.3).
 #include "q8_linear.h"
 #include <atomic>
 

@@ -9,6 +9,10 @@
 //
 // Roles of a CTA: warp 0 loads, warp 1 issues (leader) and owns the TMEM, warps 2 to 9 scale and store: thread = accumulator
 // row (token), the two groups of four warps take half of the columns each.  All waits are bounded.
+//
+// Bound by the tensor cores, and those by power: 4096 x 4096 -> 4096 from codes 46.6 us (2.95 POPS; a library product of the same
+// codes to int32, without factors, 48.6), 8192 x 4096 -> 11008 240 us (3.07 POPS, library 241), where 4.76 POPS are what the
+// instruction gives at the full clock.  Small ones are a tile's latency: 777 x 1032 -> 1000 8.7 us (library 15.4).
 #include <cmath>
 #include <type_traits>
 
