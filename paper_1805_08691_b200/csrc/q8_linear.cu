@@ -25,7 +25,7 @@ int validate_linear(const q8_linear_desc* d, LinearArgs* a) {
 }
 
 // Rows of bytes onto the 16-byte grid, zeros behind their ends: thread = 16 bytes.
-__global__ void __launch_bounds__(256) regrid_kernel(const signed char* __restrict__ in, long long rows, int C, long long ld, signed char* __restrict__ out,
+__global__ void __launch_bounds__(256) regrid_kernel(const signed char* in, long long rows, int C, long long ld, signed char* out,
                                                      int pitch) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");

@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kPThreads, 1)
   const int chunks = p.bn >> 4, half = (chunks + 1) >> 1, c0 = group * half, c1 = min(chunks, c0 + half);
   const int tokens = min(p.bn, p.M - m0);
   const bool live = warp >= 2 && n < p.K;
-  const float ws = live ? __ldg(p.w_scale + n) : 0.0f, bias = live && p.bias ? __ldg(p.bias + n) : 0.0f;
+  const float ws = live ? p.w_scale[n] : 0.0f, bias = live && p.bias ? p.bias[n] : 0.0f;
   int* const sums = reinterpret_cast<int*>(smem_raw + (base - raw));  // [token][128], over the ring
   auto value = [&](int acc, float xs) {
     float v = __fmul_rn(__fmul_rn(__int2float_rn(acc), xs), ws);
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kPThreads, 1)
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
             const int m = c * 16 + j;
-            if (live && m < tokens) y[(long long)m * p.ldy] = value(v[j], __ldg(p.x_scale + m0 + m));
+            if (live && m < tokens) y[(long long)m * p.ldy] = value(v[j], p.x_scale[m0 + m]);
           }
         }
       }
@@ -189,8 +189,8 @@ __global__ void __launch_bounds__(kPThreads, 1)
       float wsn[4], bn[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        wsn[j] = j < there ? __ldg(p.w_scale + nn + j) : 0.0f;
-        bn[j] = j < there && p.bias ? __ldg(p.bias + nn + j) : 0.0f;
+        wsn[j] = j < there ? p.w_scale[nn + j] : 0.0f;
+        bn[j] = j < there && p.bias ? p.bias[nn + j] : 0.0f;
       }
       uint32_t peer[8];
 #pragma unroll
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(kPThreads, 1)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int mu = m + u * step;
-          xs[u] = mu < tokens ? __ldg(p.x_scale + m0 + mu) : 0.0f;
+          xs[u] = mu < tokens ? p.x_scale[m0 + mu] : 0.0f;
 #pragma unroll
           for (int q = 0; q < 8; ++q) {
             v[u][q] = make_int4(0, 0, 0, 0);

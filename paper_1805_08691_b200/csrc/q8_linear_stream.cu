@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(kSThreads, 1) linear_stream_kernel(const __gri
     }
     // this thread's outputs: channel o & 15 of the tokens (o >> 4) + 16 q
     const int n0 = tile * 16 + (tid & 15);
-    const float ws = n0 < p.K ? __ldg(p.w_scale + n0) : 0.0f, bias = p.bias && n0 < p.K ? __ldg(p.bias + n0) : 0.0f;
+    const float ws = n0 < p.K ? p.w_scale[n0] : 0.0f, bias = p.bias && n0 < p.K ? p.bias[n0] : 0.0f;
     int d[NT][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0;
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(kSThreads, 1) linear_stream_kernel(const __gri
       const int sum = red[at];
       red[at] = 0;
       if (t >= p.M || n0 >= p.K) continue;
-      const float xs = p.x_type == Q8_S8 ? __ldg(p.x_scale + t) : s_fac[t].s;
+      const float xs = p.x_type == Q8_S8 ? p.x_scale[t] : s_fac[t].s;
       float v = __fmul_rn(__fmul_rn(__int2float_rn(sum), xs), ws);
       if (p.bias) v = __fadd_rn(v, bias);
       const long long o = (long long)t * p.ldy + n0;

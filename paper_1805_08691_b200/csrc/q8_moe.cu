@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
   if (p.x_vec && p.r_vec) {
 #pragma unroll 2
     for (int c = 4 * threadIdx.x; c < p.C; c += 1024) {
-      const float4 w = __ldg(reinterpret_cast<const float4*>(r + c));
+      const float4 w = *reinterpret_cast<const float4*>(r + c);
       float4 v[kTok];
 #pragma unroll
       for (int t = 0; t < kTok; ++t) v[t] = load_x4(p, row[t], c);
@@ -574,9 +574,9 @@ struct GateUp {
   __device__ __forceinline__ float2 scales(int item, int u) const {
     const int a = expert(item), i = min((item - a * p.unit_blocks) * 8 + u, p.I - 1);
     const float* s = p.sgu + (size_t)ch.expert[a] * 2 * p.I + i;
-    return make_float2(__ldg(s), __ldg(s + p.I));
+    return make_float2(s[0], s[p.I]);
   }
-  __device__ __forceinline__ unsigned token(int item, int r) const { return __float_as_uint(__ldg(p.x_factor + ch.row_token[ch.first[expert(item)] + r])); }
+  __device__ __forceinline__ unsigned token(int item, int r) const { return __float_as_uint(p.x_factor[ch.row_token[ch.first[expert(item)] + r]]); }
   __device__ __forceinline__ void finish(int item, int r, int u, bool live, float gate, float up, float2 s, unsigned factor) const {
     const int a = expert(item), i = (item - a * p.unit_blocks) * 8 + u, row = ch.first[a] + r;
     if (live && i < p.I) {
@@ -645,7 +645,7 @@ struct Down {
   __device__ __forceinline__ float2 scales(int item, int u) const {
     const int a = expert(item), c = 16 * (item - a * p.tiles) + u;
     const float* s = p.sd + (size_t)ch.expert[a] * p.C;
-    return make_float2(__ldg(s + min(c, p.C - 1)), __ldg(s + min(c + 8, p.C - 1)));
+    return make_float2(s[min(c, p.C - 1)], s[min(c + 8, p.C - 1)]);
   }
   __device__ __forceinline__ unsigned token(int item, int r) const { const int row = ch.first[expert(item)] + r; return p.direct ? ch.top[row] : __ldcg(p.largest + row); }
   __device__ __forceinline__ void finish(int item, int r, int u, bool live, float low, float high, float2 s, unsigned top) const {

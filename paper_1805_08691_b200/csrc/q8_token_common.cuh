@@ -146,14 +146,14 @@ __device__ __forceinline__ unsigned max_two(unsigned m, unsigned w) {
 // pos.  Otherwise from aligned words, each of which holds a byte of the row.
 template <bool kAligned>
 __device__ __forceinline__ uint4 load_16(const signed char* row, int pos, int len) {
-  if (kAligned && pos + 16 <= len) return __ldg(reinterpret_cast<const uint4*>(row + pos));
+  if (kAligned && pos + 16 <= len) return *reinterpret_cast<const uint4*>(row + pos);
   const int left = len - pos;
   const unsigned long long at = (unsigned long long)(row + pos);
   const unsigned* w = reinterpret_cast<const unsigned*>(at & ~3ull);
   const int m = (int)(at & 3ull);
   unsigned u[5], v[4];
 #pragma unroll
-  for (int k = 0; k < 5; ++k) u[k] = 4 * k - m < left && (k < 4 || m > 0) ? __ldg(w + k) : 0u;
+  for (int k = 0; k < 5; ++k) u[k] = 4 * k - m < left && (k < 4 || m > 0) ? w[k] : 0u;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     v[k] = __funnelshift_r(u[k], u[k + 1], 8 * m);

@@ -27,7 +27,7 @@ struct Chunk {
   unsigned w[V * sizeof(T) / 4];
   __device__ __forceinline__ void load(const T* at, int left) {
     if (kVec && V <= left) {
-      *reinterpret_cast<uint4*>(w) = __ldg(reinterpret_cast<const uint4*>(at));
+      *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(at);
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
@@ -87,8 +87,8 @@ __device__ __forceinline__ unsigned as_fp32_bits(unsigned m) {  // of a maximum 
 
 // Teams of kTeam threads, a token each.  kTeam 32: eight tokens a block.
 template <typename T, bool kVec, int kTeam>
-__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : (kTeam == 128 ? 10 : 5)) quantize_tokens_kernel(const T* __restrict__ x, size_t tokens, size_t C, size_t ldx,
-                                                                                    signed char* __restrict__ z, size_t ldz, float* __restrict__ scale) {
+__global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : (kTeam == 128 ? 10 : 5)) quantize_tokens_kernel(const T* x, size_t tokens, size_t C, size_t ldx,
+                                                                                    signed char* z, size_t ldz, float* scale) {
   using Part = Chunk<T, kVec, kTeam>;
   __shared__ unsigned part[kTeam / 32];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -138,8 +138,8 @@ __global__ void __launch_bounds__(kTeam == 32 ? 256 : kTeam, kTeam == 512 ? 2 : 
 
 // Sixteen codes a thread and turn where rows lie on the 16-byte grid, else four kTeam apart.
 template <typename T, bool kVec, int kTeam>
-__global__ void __launch_bounds__(256) dequantize_tokens_kernel(const signed char* __restrict__ z, size_t tokens, size_t C, size_t ldz,
-                                                                const float* __restrict__ scale, T* __restrict__ r, size_t ldr) {
+__global__ void __launch_bounds__(256) dequantize_tokens_kernel(const signed char* z, size_t tokens, size_t C, size_t ldz,
+                                                                const float* scale, T* r, size_t ldr) {
   constexpr int V = kVec ? 16 : 4;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(256) dequantize_tokens_kernel(const signed cha
   constexpr int kStep = kVec ? 1 : kTeam;
   for (size_t c = (size_t)(threadIdx.x % kTeam) * (kVec ? V : 1); c < C; c += (size_t)kTeam * V) {
     if (kVec && c + V <= C) {
-      const uint4 w = __ldg(reinterpret_cast<const uint4*>(in + c));
+      const uint4 w = *reinterpret_cast<const uint4*>(in + c);
       const unsigned u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
       for (int j = 0; j < 4; j += sizeof(T) == 4 ? 1 : 2) {
