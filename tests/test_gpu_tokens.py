@@ -491,6 +491,62 @@ def test_two_graphs_share_a_workspace(q8):
             assert all(torch.equal(a, b) for a, b in zip(o, want))
 
 
+def test_weights_past_32_bits(q8):
+    C, K = 8192, 300000
+    w = torch.empty(K, C, dtype=torch.int8, device="cuda")
+    w.random_(-128, 128, generator=_gen(110))
+    ws = torch.rand(K, generator=_gen(111), device="cuda")
+    for M in (1, 12, 40, 300):
+        x = _acts(112 + M, M, C, dtype=torch.float16)
+        y = q8.q8_linear(x, w, ws)
+        for at in (0, 262143, K - 260):
+            assert torch.equal(y[:, at:at + 260], q8.q8_linear(x, w[at:at + 260], ws[at:at + 260])), (M, at)
+    del w
+    C, I, E, k = 4096, 2100, 160, 2
+    g = _gen(113)
+    wgu = torch.empty(E, 2 * I, C, dtype=torch.int8, device="cuda").random_(-128, 128, generator=g)
+    wd = torch.empty(E, C, I, dtype=torch.int8, device="cuda").random_(-128, 128, generator=g)
+    sgu, sd = torch.rand(E, 2 * I, generator=g, device="cuda") / 4096, torch.rand(E, C, generator=g, device="cuda") / 4096
+    router = torch.zeros(E, C, device="cuda")
+    router[E - 1], router[E - 2], router[0] = 1.0 / C, 0.99 / C, 0.98 / C
+    for T in (1, 3, 6):
+        x = _acts(114, T, C).abs()
+        got = q8.q8_moe(x, router, wgu, sgu, wd, sd, k)
+        assert got[1].tolist() == [[E - 1, E - 2]] * T
+        check_moe(got, plain_moe(x, router, wgu, sgu, wd, sd, k, True))
+    q8.q8_read_status()
+
+
+@pytest.mark.parametrize("T", [1, 6])
+def test_moe_of_bad_weights_ends(q8, T):
+    """Every NaN is a value like others: also the one of all ones, in a factor, and nobody waits for what is behind it."""
+    C, I, E, k = 128, 80, 4, 2
+    x = _acts(120, T, C)
+    router, wgu, sgu, wd, sd = _experts(121, C, I, E)
+    router[:] = 0
+    router[1], router[2] = 1e-3 * x.sum(0), 1e-3 * x.sum(0)
+    want = q8.q8_moe(x, router, wgu, sgu, wd, sd, E, renormalize=True)
+    ones = torch.full((1,), -1, dtype=torch.int32, device="cuda").view(torch.float32)
+    bad = sd.clone()
+    bad[1, 5], bad[2, 7], bad[3, 127] = ones[0], float("inf"), float("nan")
+    y = q8.q8_moe(x, router, wgu, sgu, wd, bad, E)[0]
+    gone = torch.zeros(C, dtype=torch.bool, device="cuda")
+    gone[[5, 7, 127]] = True
+    assert bool((~torch.isfinite(y[:, gone])).all()) and torch.equal(y[:, ~gone], want[0][:, ~gone])
+    for value in (ones[0], float("nan"), float("inf")):
+        bad = sgu.clone()
+        bad[2, 3] = value
+        y = q8.q8_moe(x, router, wgu, bad, wd, sd, E)[0]
+        assert bool(torch.isnan(y).all())
+    q8.q8_read_status()
+
+
+def test_moe_without_tokens(q8):
+    router, *rest = _experts(122, 64, 32, 4)
+    y, ids, probs = q8.q8_moe(torch.empty(0, 64, device="cuda"), router, *rest, 2)
+    assert y.shape == (0, 64) and ids.shape == (0, 2) and probs.shape == (0, 2)
+
+
 # ------------------------------------------------------------------------------------------------ as they are used
 def test_prepared_layers(q8):
     from paper_1805_08691_b200 import pipeline
