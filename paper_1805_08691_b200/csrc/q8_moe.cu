@@ -595,7 +595,7 @@ struct Down {
   int *known, *gave_up;    // (shared memory) see wait_block
   signed char* mine;       // shared memory of this warp for an item's digits
   int warp, warps;
-  mutable bool looked;
+  mutable bool looked, all;  // whether this warp has looked (or waited), and whether it knows all rows
   // The warps of a block share the rows whose largest magnitudes it needs.  (Called with the first weights on their way.)
   __device__ __forceinline__ void look(int lane) const {
     if (looked || !p.direct) return;
@@ -622,7 +622,8 @@ struct Down {
   __device__ __forceinline__ void columns(int item, int count, int s0, int n, int lane, const signed char* (&z)[NT]) const {
     const int a = expert(item), first = ch.first[a], digit = (lane >> 2) & 3;
     if (!p.direct) {
-      wait_block(&p.sync[kDoneRows], (unsigned)(p.T * p.k), known, gave_up, p.status);
+      if (!looked) wait_block(&p.sync[kDoneRows], (unsigned)(p.T * p.k), known, gave_up, p.status);
+      looked = true;
       const signed char* from = p.hd + (size_t)first * 4 * p.h_pitch + 64 * s0 + 16 * (lane & 3);
 #pragma unroll
       for (int t = 0; t < NT; ++t) z[t] = from + (size_t)(min(2 * t + (lane >> 4), count - 1) * 4 + digit) * p.h_pitch;
@@ -632,10 +633,19 @@ struct Down {
     const int pitch = staged_pitch(n);
     __syncwarp();  // (all lanes have read what was there)
     look(lane);
+    const volatile unsigned* tops = ch.top;
+    if (!all) {
+      bool absent = false;
+      for (int r = lane; r < p.T * p.k; r += 32) absent |= tops[r] == kAbsent;
+      all = !__any_sync(0xffffffffu, absent);
+      if (all) __threadfence_block();
+    }
     for (int r = 0; r < count; ++r) {
-      unsigned top;
-      while (!__all_sync(0xffffffffu, (top = *const_cast<volatile unsigned*>(ch.top + first + r)) != kAbsent)) __nanosleep(20);  // (who looks stops in time)
-      __threadfence_block();
+      unsigned top = tops[first + r];
+      if (!all) {
+        while (!__all_sync(0xffffffffu, (top = tops[first + r]) != kAbsent)) __nanosleep(20);  // (who looks stops in time)
+        __threadfence_block();
+      }
       make_digits(p, first + r, top, 64 * s0, 64 * n, mine + 4 * r * pitch, pitch, lane);
     }
     __syncwarp();
@@ -842,7 +852,7 @@ __global__ void __launch_bounds__(32 * warps_of(NT), 1) moe_experts_kernel(const
     }
   }
   __syncthreads();
-  const Down job{p, ch, &s_known, &gave_up, own, warp, kMoeWarps, false};
+  const Down job{p, ch, &s_known, &gave_up, own, warp, kMoeWarps, false, false};
   run_phase<NT, kGrid, kLater>(job, items2, (p.I + 63) >> 6, p.ks[1], &p.sync[kBlocks2], s_block[1], s_next, acc, ring2, lane, warp);
   job.look(lane);  // (of a warp without an item)
   // ---- the results, a warp sixteen channels of two tokens
