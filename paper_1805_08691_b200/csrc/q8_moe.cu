@@ -3,7 +3,7 @@
 // Few tokens read each chosen expert's weights once and do little else: the layer is bound by the bytes of the weights, and
 // everything between two streams of them is latency.  Two kernels:
 //
-//   moe_route_kernel    logits in 64 bits, a block per expert and four tokens; the tokens as integer digits, a block each;
+//   moe_route_kernel    logits in 64 bits, a block per expert and up to four tokens; the tokens as integer digits, a block each;
 //   moe_experts_kernel  all the rest.  Every block finds the chosen experts itself.  Then warps draw items by tickets: first
 //                       of eight inner units (their eight gate and eight up rows are the sixteen rows of an instruction),
 //                       then of sixteen output channels of an expert.
@@ -27,9 +27,9 @@
 // on their way, and with every item it waits for in the hands of a running warp: progress needs no co-residency.  Waits are
 // bounded all the same.
 //
-// 1 token 2048 x 768, 8 of 64 experts 22 us, of which the weights' bytes are 6; 2 tokens 4096 x 2048, 2 of 8 experts 36 us (14);
-// 16 tokens 2048 x 1024, 8 of 64 experts 97 us (55); 8 tokens 4096 x 1536, 8 of 128 experts 203 us (151).  What is left is a chain
-// of latencies: two launches and the router 8 us, the choice 3, the first reads of either phase and what lies between them.
+// 1 token 2048 x 768, 8 of 64 experts 20.7 us, of which the weights' bytes are 6; 2 tokens 4096 x 2048, 2 of 8 experts 35 us
+// (14); 16 tokens 2048 x 1024, 8 of 64 experts 96 us (55); 8 tokens 4096 x 1536, 8 of 128 experts 203 us (151).  What is left is a
+// chain of latencies: two launches and the router 7 us, the choice 3, the first reads of either phase and what lies between them.
 #include <atomic>
 #include <cmath>
 #include <type_traits>
@@ -148,7 +148,7 @@ __device__ __forceinline__ float digits_sum(int high, int low) { return __fmaf_r
 
 // ------------------------------------------------------------------------------------------ router
 template <int kTok>
-__global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ MoeParams p) {
+__global__ void __launch_bounds__(256, 2) moe_route_kernel(const __grid_constant__ MoeParams p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -162,24 +162,8 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
     const int t = blockIdx.x;
     if (t == 0) for (int i = threadIdx.x; i < kCounters; i += 256) p.sync[i] = 0u;
     __shared__ unsigned part[8];
-    unsigned m = 0;
-    if (p.x_vec) {
-      for (int c = 4 * threadIdx.x; c < p.C; c += 1024) {
-        const float4 v = load_x4(p, t, c);
-        m = max(m, max(max(abs_word(v.x), abs_word(v.y)), max(abs_word(v.z), abs_word(v.w))));
-      }
-    } else {
-      for (int c = threadIdx.x; c < p.C; c += 256) m = max(m, abs_word(load_x(p, t, c)));
-    }
-    m = warp_max(m);
-    if (lane == 0) part[warp] = m;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, part[i]);
-    const DigitScale s = digit_scale(m);
-    if (threadIdx.x == 0) p.x_factor[t] = s.factor;
-    signed char* out = p.xd + (size_t)t * 4 * p.x_pitch;
-    for (int c = 4 * threadIdx.x; c < p.x_pitch; c += 1024) {
+    // four pieces of four values a thread at a time, on their way together; the first four stay
+    auto load = [&](int c) {
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (p.x_vec) {
         if (c < p.C) v = load_x4(p, t, c);
@@ -189,14 +173,40 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
         if (c + 2 < p.C) v.z = load_x(p, t, c + 2);
         if (c + 3 < p.C) v.w = load_x(p, t, c + 3);
       }
+      return v;
+    };
+    auto top = [](const float4& v) { return max(max(abs_word(v.x), abs_word(v.y)), max(abs_word(v.z), abs_word(v.w))); };
+    const int c0 = 4 * threadIdx.x;
+    float4 held[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) held[j] = load(c0 + 1024 * j);
+    unsigned m = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m = max(m, top(held[j]));
+#pragma unroll 4
+    for (int c = c0 + 4096; c < p.C; c += 1024) m = max(m, top(load(c)));
+    m = warp_max(m);
+    if (lane == 0) part[warp] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, part[i]);
+    const DigitScale s = digit_scale(m);
+    if (threadIdx.x == 0) p.x_factor[t] = s.factor;
+    signed char* out = p.xd + (size_t)t * 4 * p.x_pitch;
+    auto put = [&](int c, const float4& v) {
       unsigned d[4];
       digits_4(v, s, d);
 #pragma unroll
       for (int j = 0; j < 4; ++j) *reinterpret_cast<unsigned*>(out + j * (size_t)p.x_pitch + c) = d[j];
-    }
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (c0 + 1024 * j < p.x_pitch) put(c0 + 1024 * j, held[j]);
+    for (int c = c0 + 4096; c < p.x_pitch; c += 1024) put(c, load(c));
     return;
   }
   // an expert's logits of kTok tokens; a thread's share of the channels does not depend on their number
+  constexpr int kAt = kTok > 2 ? 2 : 4;
   __shared__ double part_sum[8][kTok];
   const int index = (int)blockIdx.x - p.T, e = index % p.E, t0 = index / p.E * kTok;
   const float* r = p.router + (size_t)e * p.C;
@@ -205,19 +215,25 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
 #pragma unroll
   for (int t = 0; t < kTok; ++t) { s[t] = 0.0; row[t] = min(t0 + t, p.T - 1); }
   if (p.x_vec && p.r_vec) {
-#pragma unroll 2
-    for (int c = 4 * threadIdx.x; c < p.C; c += 1024) {
-      const float4 w = *reinterpret_cast<const float4*>(r + c);
-      float4 v[kTok];
+    for (int c0 = 4 * threadIdx.x; c0 < p.C; c0 += 1024 * kAt) {  // kAt pieces on their way together
+      float4 w[kAt], v[kAt][kTok];
 #pragma unroll
-      for (int t = 0; t < kTok; ++t) v[t] = load_x4(p, row[t], c);
+      for (int j = 0; j < kAt; ++j) {
+        const int c = c0 + 1024 * j;
+        const bool live = c < p.C;
+        w[j] = live ? *reinterpret_cast<const float4*>(r + c) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int t = 0; t < kTok; ++t) {
-        s[t] = __fma_rn((double)v[t].x, (double)w.x, s[t]);
-        s[t] = __fma_rn((double)v[t].y, (double)w.y, s[t]);
-        s[t] = __fma_rn((double)v[t].z, (double)w.z, s[t]);
-        s[t] = __fma_rn((double)v[t].w, (double)w.w, s[t]);
+        for (int t = 0; t < kTok; ++t) v[j][t] = live ? load_x4(p, row[t], c) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
+#pragma unroll
+      for (int j = 0; j < kAt; ++j)
+#pragma unroll
+        for (int t = 0; t < kTok; ++t) {
+          s[t] = __fma_rn((double)v[j][t].x, (double)w[j].x, s[t]);
+          s[t] = __fma_rn((double)v[j][t].y, (double)w[j].y, s[t]);
+          s[t] = __fma_rn((double)v[j][t].z, (double)w[j].z, s[t]);
+          s[t] = __fma_rn((double)v[j][t].w, (double)w[j].w, s[t]);
+        }
     }
   } else {
 #pragma unroll 2
@@ -227,13 +243,23 @@ __global__ void __launch_bounds__(256) moe_route_kernel(const __grid_constant__ 
       for (int t = 0; t < kTok; ++t) s[t] = __fma_rn((double)load_x(p, row[t], c), w, s[t]);
     }
   }
+  // the same pairs are added for any kTok; with several tokens a lane gives half of them away and keeps the others
+  int mine = 0;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
+  for (int o = 16, n = kTok / 2; o > 0; o >>= 1, n /= 2) {
+    if (n > 0) {
+      const bool upper = lane & o;
 #pragma unroll
-    for (int t = 0; t < kTok; ++t) s[t] += __shfl_xor_sync(0xffffffffu, s[t], o);
-#pragma unroll
-  for (int t = 0; t < kTok; ++t)
-    if (lane == 0) part_sum[warp][t] = s[t];
+      for (int t = 0; t < n; ++t) {
+        const double away = __shfl_xor_sync(0xffffffffu, upper ? s[t] : s[t + n], o);
+        s[t] = (upper ? s[t + n] : s[t]) + away;
+      }
+      if (upper) mine += n;
+    } else {
+      s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
+    }
+  }
+  if ((lane & (32 / kTok - 1)) == 0) part_sum[warp][mine] = s[0];
   __syncthreads();
   if ((int)threadIdx.x < kTok && t0 + (int)threadIdx.x < p.T) {
     double l = part_sum[0][threadIdx.x];
@@ -953,7 +979,7 @@ int launch_experts(const MoeParams& p, cudaStream_t s) {
 }
 
 int launch_route(const MoeParams& p, cudaStream_t s) {
-  const int per = p.T == 1 ? 1 : 4;  // tokens of a block
+  const int per = p.T <= 2 ? p.T : 4;  // tokens of a block
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(p.T + p.E * ((p.T + per - 1) / per)));
   cfg.blockDim = dim3(256);
@@ -963,7 +989,7 @@ int launch_route(const MoeParams& p, cudaStream_t s) {
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return check_cuda(cudaLaunchKernelEx(&cfg, per == 1 ? moe_route_kernel<1> : moe_route_kernel<4>, p), "moe_route_kernel");
+  return check_cuda(cudaLaunchKernelEx(&cfg, per == 1 ? moe_route_kernel<1> : (per == 2 ? moe_route_kernel<2> : moe_route_kernel<4>), p), "moe_route_kernel");
 }
 
 }  // namespace
